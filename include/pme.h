@@ -205,6 +205,61 @@ pme_status pme_expanded_linear_mxfp4(const void* x, pme_dtype xt, int64_t T, int
                                      void* y_bf16, int64_t ldy, void* workspace, size_t workspace_bytes,
                                      void* stream);
 
+/*
+ * ---- 8-bit layers around the expanded projection ----
+ *
+ * The products that feed the down projection of pme_expanded_linear* (Section 4 quantizes every linear layer; the ones
+ * that are not expanded can be kept in 8 bits): codes in e4m3 (OCP FP8: sign, 4 exponent and 3 mantissa bits, largest
+ * value 448, no infinities) with an fp32 scale for each block of 128, value = scale * code.
+ *
+ *  - Activations: a scale for each token and 128 consecutive features; weights: one for each block of 128 output
+ *    channels x 128 features.  scale = amax / 448 over the block, at least 2^-126, 1 where the block is all zeros; code =
+ *    e4m3(v / scale), round half to even.  A block that holds a NaN or an infinity gets a NaN scale and NaN codes.
+ *  - Rows of codes are dense and hold whole blocks: Kp = 128 ceil(d / 128) bytes, the codes beyond d are 0.  Scales are
+ *    dense, [rows, Kp / 128].  Codes are 16-byte aligned, scales 4-byte aligned (PME_ERR_ALIGN).
+ *  - T == 0 or N == 0 is a no-op.  No call needs a workspace or a first call outside a graph's capture.
+ */
+
+/*
+ * Residual addition, root-mean-square norm and quantization of the result:
+ *   h = x + residual, rounded to xt;  v[t][j] = h[t][j] (mean_j h[t][j]^2 + eps)^-1/2 weight[j];  qx, sx = codes of v.
+ *   x, residual, h  DEVICE [T, d] row-major of type xt, pitches ldx, ldr, ldh >= d (elements).  residual may be NULL:
+ *       then h must be NULL too, and h = x is not written.  h may be x or residual itself (the same pointer and pitch),
+ *       and must not overlap them otherwise.
+ *   weight  DEVICE [d] of type wt.   eps >= 0 and finite (PME_ERR_SHAPE).
+ *   qx  DEVICE out [T, Kp],  sx  DEVICE out [T, Kp / 128].
+ * The sum of squares is taken in fp32, again on scaled values where it leaves fp32's range, so that values of any
+ * magnitude give the quotients above (a row of zeros gives zeros).  A row that holds a NaN or an infinity comes out as
+ * NaN.  Alignment: x, residual, h and weight to their element size.
+ */
+pme_status pme_rmsnorm_quant_fp8(const void* x, pme_dtype xt, int64_t T, int64_t d, int64_t ldx, const void* residual,
+                                 int64_t ldr, void* h, int64_t ldh, const void* weight, pme_dtype wt, float eps,
+                                 uint8_t* qx, float* sx, void* stream);
+
+/* Activations that come from elsewhere than a norm: qx, sx = codes of x.  Arguments as above. */
+pme_status pme_quant_fp8(const void* x, pme_dtype xt, int64_t T, int64_t d, int64_t ldx, uint8_t* qx, float* sx, void* stream);
+
+/* Offline weight side: wt DEVICE [N, d] row-major (one row per output channel), ldw elements between rows ->
+ * qw DEVICE out [N, Kp], sw DEVICE out [ceil(N / 128), Kp / 128]. */
+pme_status pme_quantize_weights_fp8(const void* wt, pme_dtype wtype, int64_t N, int64_t d, int64_t ldw, uint8_t* qw, float* sw,
+                                    void* stream);
+
+/*
+ * y[t][n] = bf16( sum_g sx[t][g] sw[n / 128][g] sum_{k in block g} qx[t][k] qw[n][k] ), accumulated in fp32.
+ *   qx DEVICE [T, K], sx DEVICE [T, K / 128]; qw DEVICE [N, K], sw DEVICE [ceil(N / 128), K / 128]; K a multiple of 128
+ *   (Kp above).  y DEVICE out [T, N] bf16 row-major, ldy elements between rows (ldy >= N), 2-byte aligned.
+ */
+pme_status pme_fp8_gemm(const uint8_t* qx, const float* sx, const uint8_t* qw, const float* sw, int64_t T, int64_t K, int64_t N,
+                        void* y_bf16, int64_t ldy, void* stream);
+
+/*
+ * Both projections of a gated feed-forward block, its activation and the product of the two in one kernel:
+ *   y[t][n] = bf16( g / (1 + e^-g) * u ),  g and u the products of pme_fp8_gemm with (qg, sg) and (qu, su), in fp32.
+ * y is the input of the block's down projection (pme_expanded_linear*).
+ */
+pme_status pme_fp8_gated_gemm(const uint8_t* qx, const float* sx, const uint8_t* qg, const float* sg, const uint8_t* qu, const float* su,
+                              int64_t T, int64_t K, int64_t N, void* y_bf16, int64_t ldy, void* stream);
+
 /* Bytes of workspace the pme_expanded_linear* calls need for the quantized activations of Section 3's Q(X H_hat):
  * packed codes [T, d_e/2], per-token scales (or MXFP4 scale bytes) and zero points, each part 256-byte aligned
  * (one size serves all three calls; 0 on invalid sizes).  N is accepted for symmetry and does not enter. */
@@ -276,6 +331,9 @@ void pme_set_gemm_tile(int id);
  * terminating zero.  Nothing is launched.  The benchmark uses it to check that stored profiler figures belong to
  * the kernel it is timing. */
 pme_status pme_gemm_plan(int variant, int64_t T, int64_t d_e, int64_t N, char* name, size_t name_len);
+
+/* The same of pme_fp8_gemm (gated = 0) and pme_fp8_gated_gemm (gated != 0). */
+pme_status pme_fp8_gemm_plan(int gated, int64_t T, int64_t K, int64_t N, char* name, size_t name_len);
 
 void pme_set_path(pme_path p);
 pme_path pme_get_path(void);

@@ -18,6 +18,7 @@ EXPORTS = ("pme_hadamard_expand_quant", "pme_expand_quantize_weights", "pme_hada
            "pme_mxfp4_gemm", "pme_expanded_linear_mxfp4", "pme_hadamard_expand_quant_asym", "pme_w4a4_gemm", "pme_w4a4_gemm_asym",
            "pme_weight_rowsum", "pme_expanded_linear", "pme_expanded_linear_static", "pme_expanded_linear_asym", "pme_workspace_bytes", "pme_hadamard_expand_f32",
            "pme_w4a4_gemm_i32", "pme_factor_order", "pme_base_block", "pme_pack_int4", "pme_gemm_plan", "pme_probe_copy", "pme_probe_read", "pme_probe_launch", "pme_probe_mfma",
+           "pme_rmsnorm_quant_fp8", "pme_quant_fp8", "pme_quantize_weights_fp8", "pme_fp8_gemm", "pme_fp8_gated_gemm", "pme_fp8_gemm_plan",
            "pme_set_path", "pme_set_gemm_tile",
            "pme_get_path", "pme_status_string", "pme_version")
 
@@ -61,6 +62,12 @@ def lib() -> C.CDLL:
     L.pme_base_block.argtypes = [i64, vp]
     L.pme_pack_int4.argtypes = [vp, i64, i64, vp, vp]
     L.pme_gemm_plan.argtypes = [i32, i64, i64, i64, C.c_char_p, sz]
+    L.pme_rmsnorm_quant_fp8.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp, i32, C.c_float, vp, vp, vp]
+    L.pme_quant_fp8.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+    L.pme_quantize_weights_fp8.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
+    L.pme_fp8_gemm.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, i64, vp]
+    L.pme_fp8_gated_gemm.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, i64, vp]
+    L.pme_fp8_gemm_plan.argtypes = [i32, i64, i64, i64, C.c_char_p, sz]
     L.pme_probe_copy.argtypes = [vp, vp, sz, vp]
     L.pme_probe_read.argtypes = [vp, sz, vp, sz, vp]
     L.pme_probe_launch.argtypes = [vp]
@@ -309,6 +316,134 @@ def expanded_linear(x, d_e: int, qw, sw, y: torch.Tensor | None = None, workspac
                                      _dev(workspace, "workspace"), workspace.numel() * workspace.element_size(),
                                      _stream()), "pme_expanded_linear")
     return y
+
+
+# ---- 8-bit layers: e4m3 codes (torch.float8_e4m3fn, rows of whole groups of 128) with a float32 scale for each block of 128 ----
+
+FP8_BLOCK = 128
+_FP8 = torch.float8_e4m3fn
+
+
+def _here(*tensors) -> int:
+    """The device all of `tensors` are on, which has to be the current one (the launches go to its current stream)."""
+    dev = torch.cuda.current_device() if tensors[0].is_cuda else -1
+    for t in tensors:
+        if not t.is_cuda or t.get_device() != dev:
+            raise ValueError("every operand must be a tensor of the current device")
+    return dev
+
+
+def _codes_out(q, s, rows: int, srows: int, d: int, device):
+    groups = (d + FP8_BLOCK - 1) // FP8_BLOCK
+    if q is None:
+        q = torch.empty((rows, groups * FP8_BLOCK), dtype=_FP8, device=device)
+    elif q.dtype != _FP8 or q.shape != (rows, groups * FP8_BLOCK) or not q.is_contiguous():
+        raise ValueError(f"the codes must be a contiguous float8_e4m3fn [{rows}, {groups * FP8_BLOCK}] tensor")
+    if s is None:
+        s = torch.empty((srows, groups), dtype=torch.float32, device=device)
+    elif s.dtype != torch.float32 or s.shape != (srows, groups) or not s.is_contiguous():
+        raise ValueError(f"the scales must be a contiguous float32 [{srows}, {groups}] tensor")
+    return q, s
+
+
+def rmsnorm_quant_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor | None = None,
+                      h: torch.Tensor | None = None, qx: torch.Tensor | None = None, sx: torch.Tensor | None = None):
+    """Codes and scales of the root-mean-square norm of x, or of h = x + residual when a residual is given
+    -> (qx, sx), or (qx, sx, h).  h may be x or residual itself."""
+    T, d, ldx = _rows(x)
+    xt, wt = _dtype_code(x), _dtype_code(weight)
+    if weight.dim() != 1 or weight.shape[0] != d or not weight.is_contiguous():
+        raise ValueError("weight must be a contiguous [d] tensor")
+    if residual is None:
+        if h is not None:
+            raise ValueError("h is the sum with a residual: give both or neither")
+        qx, sx = _codes_out(qx, sx, T, T, d, x.device)
+        _here(x, weight, qx, sx)
+        _check(lib().pme_rmsnorm_quant_fp8(x.data_ptr(), xt, T, d, ldx, None, 0, None, 0, weight.data_ptr(), wt, eps,
+                                           qx.data_ptr(), sx.data_ptr(), _stream()), "pme_rmsnorm_quant_fp8")
+        return qx, sx
+    if h is None:
+        h = torch.empty((T, d), dtype=x.dtype, device=x.device)
+    if residual.dtype != x.dtype or h.dtype != x.dtype or residual.shape != x.shape or h.shape != x.shape:
+        raise ValueError("residual and h must have x's shape and type")
+    ldr, ldh = _rows(residual)[2], _rows(h)[2]
+    qx, sx = _codes_out(qx, sx, T, T, d, x.device)
+    _here(x, residual, h, weight, qx, sx)
+    _check(lib().pme_rmsnorm_quant_fp8(x.data_ptr(), xt, T, d, ldx, residual.data_ptr(), ldr, h.data_ptr(), ldh,
+                                       weight.data_ptr(), wt, eps, qx.data_ptr(), sx.data_ptr(), _stream()),
+           "pme_rmsnorm_quant_fp8")
+    return qx, sx, h
+
+
+def quant_fp8(x: torch.Tensor, qx: torch.Tensor | None = None, sx: torch.Tensor | None = None):
+    """Codes and scales of activations [T, d], a scale for each token and group of 128 features -> (qx, sx)."""
+    T, d, ldx = _rows(x)
+    xt = _dtype_code(x)
+    qx, sx = _codes_out(qx, sx, T, T, d, x.device)
+    _here(x, qx, sx)
+    _check(lib().pme_quant_fp8(x.data_ptr(), xt, T, d, ldx, qx.data_ptr(), sx.data_ptr(), _stream()), "pme_quant_fp8")
+    return qx, sx
+
+
+def quantize_weights_fp8(wt: torch.Tensor, qw: torch.Tensor | None = None, sw: torch.Tensor | None = None):
+    """Codes and scales of weights [N, d] (torch Linear layout), a scale for each block of 128 x 128 -> (qw, sw)."""
+    N, d, ldw = _rows(wt)
+    code = _dtype_code(wt)
+    qw, sw = _codes_out(qw, sw, N, (N + FP8_BLOCK - 1) // FP8_BLOCK, d, wt.device)
+    _here(wt, qw, sw)
+    _check(lib().pme_quantize_weights_fp8(wt.data_ptr(), code, N, d, ldw, qw.data_ptr(), sw.data_ptr(), _stream()),
+           "pme_quantize_weights_fp8")
+    return qw, sw
+
+
+def _fp8_operand(q, s, what: str, per: int):
+    if q.dim() != 2 or q.dtype != _FP8 or not q.is_contiguous() or q.shape[1] % FP8_BLOCK:
+        raise ValueError(f"q{what} must be a contiguous float8_e4m3fn tensor with rows of whole groups of 128")
+    rows, K = q.shape
+    if s.dtype != torch.float32 or s.shape != ((rows + per - 1) // per, K // FP8_BLOCK) or not s.is_contiguous():
+        raise ValueError(f"s{what} must be a contiguous float32 tensor with one scale for each block of q{what}")
+    return rows, K
+
+
+def _fp8_out(y, T: int, N: int, device):
+    if y is None:
+        return torch.empty((T, N), dtype=torch.bfloat16, device=device), N
+    if y.dtype != torch.bfloat16 or y.shape != (T, N) or (N > 1 and y.stride(1) != 1):
+        raise ValueError(f"y must be a bfloat16 [{T}, {N}] tensor with unit stride along its rows")
+    return y, y.stride(0) if T > 1 else max(y.stride(0), N)
+
+
+def fp8_gemm(qx, sx, qw, sw, y: torch.Tensor | None = None) -> torch.Tensor:
+    """y [T, N] = product of activations (qx [T, K], sx [T, K/128]) and weights (qw [N, K], sw [ceil(N/128), K/128])."""
+    T, K = _fp8_operand(qx, sx, "x", 1)
+    N, Kw = _fp8_operand(qw, sw, "w", FP8_BLOCK)
+    if Kw != K:
+        raise ValueError("qx and qw disagree on K")
+    y, ldy = _fp8_out(y, T, N, qx.device)
+    _here(qx, sx, qw, sw, y)
+    _check(lib().pme_fp8_gemm(qx.data_ptr(), sx.data_ptr(), qw.data_ptr(), sw.data_ptr(), T, K, N, y.data_ptr(), ldy, _stream()),
+           "pme_fp8_gemm")
+    return y
+
+
+def fp8_gated_gemm(qx, sx, qg, sg, qu, su, y: torch.Tensor | None = None) -> torch.Tensor:
+    """y [T, N] = silu(g) * u, g and u the products of the activations with the gate's and the other projection's weights."""
+    T, K = _fp8_operand(qx, sx, "x", 1)
+    N, Kg = _fp8_operand(qg, sg, "g", FP8_BLOCK)
+    if _fp8_operand(qu, su, "u", FP8_BLOCK) != (N, K) or Kg != K:
+        raise ValueError("qx, qg and qu disagree on K, or qg and qu on N")
+    y, ldy = _fp8_out(y, T, N, qx.device)
+    _here(qx, sx, qg, sg, qu, su, y)
+    _check(lib().pme_fp8_gated_gemm(qx.data_ptr(), sx.data_ptr(), qg.data_ptr(), sg.data_ptr(), qu.data_ptr(), su.data_ptr(),
+                                    T, K, N, y.data_ptr(), ldy, _stream()), "pme_fp8_gated_gemm")
+    return y
+
+
+def fp8_gemm_plan(T: int, K: int, N: int, gated: bool = False) -> str:
+    """Name of the kernel instantiation fp8_gemm (or fp8_gated_gemm) of this shape would run, as a profiler prints it."""
+    buf = C.create_string_buffer(128)
+    _check(lib().pme_fp8_gemm_plan(int(gated), T, K, N, buf, len(buf)), "pme_fp8_gemm_plan")
+    return buf.value.decode()
 
 
 STATIC_SCRATCH_BYTES = 16 << 20

@@ -185,6 +185,51 @@ template <class Gemm> pme_status run_layer(const pme::RotateArgs& ra, const Gemm
     return run(ga);
 }
 
+// Products of e4m3 codes: whole blocks of 128 codes, operands of 16-byte aligned rows.
+pme_status check_fp8_gemm(const pme::Fp8GemmArgs& a, bool gated) {
+    if (a.T < 0 || a.N < 0 || a.K <= 0 || a.K % 128 || a.ldy < a.N) return PME_ERR_SHAPE;
+    if (a.T > 0x7FFFFFFF || a.N > 0x7FFFFFFF || a.K > (int64_t(1) << 20)) return PME_ERR_SHAPE;
+    if (a.T > 0 && a.N > 0 && (!a.qx || !a.sx || !a.qw || !a.sw || !a.y || (gated && (!a.qu || !a.su)))) return PME_ERR_NULL;
+    if (!aligned(a.qx, 16) || !aligned(a.qw, 16) || !aligned(a.qu, 16) || !aligned(a.sx, 4) || !aligned(a.sw, 4) || !aligned(a.su, 4) || !aligned(a.y, 2))
+        return PME_ERR_ALIGN;
+    return PME_OK;
+}
+
+pme_status run_fp8_gemm_slice(const pme::Fp8GemmArgs& a) { return pme::launch_fp8_gemm_generic(a); }
+
+pme_status run_fp8_gemm(const pme::Fp8GemmArgs& a) {
+    if (a.T == 0 || a.N == 0) return PME_OK;
+    const int64_t rows = max_slice_rows(a.K), groups = a.K / 128;
+    if (a.T <= rows && a.N <= rows) return run_fp8_gemm_slice(a);
+    for (int64_t t0 = 0; t0 < a.T; t0 += rows)
+        for (int64_t n0 = 0; n0 < a.N; n0 += rows) {        // a multiple of 128: a slice starts with a block of scales
+            pme::Fp8GemmArgs p = a;
+            p.T = std::min(rows, a.T - t0);
+            p.N = std::min(rows, a.N - n0);
+            p.qx = a.qx + t0 * a.K;
+            p.sx = a.sx + t0 * groups;
+            p.qw = a.qw + n0 * a.K;
+            p.sw = a.sw + n0 / 128 * groups;
+            if (a.qu) {
+                p.qu = a.qu + n0 * a.K;
+                p.su = a.su + n0 / 128 * groups;
+            }
+            p.y = static_cast<unsigned char*>(a.y) + (t0 * a.ldy + n0) * 2;
+            const pme_status s = run_fp8_gemm_slice(p);
+            if (s != PME_OK) return s;
+        }
+    return PME_OK;
+}
+
+// A quantizer's input of rows x d values and its codes and scales.
+pme_status check_quant_fp8(const void* x, pme_dtype xt, int64_t rows, int64_t d, int64_t ldx, const uint8_t* q, const float* s) {
+    if (xt != PME_F32 && xt != PME_BF16) return PME_ERR_DTYPE;
+    if (rows < 0 || d <= 0 || ldx < d || rows > 0x7FFFFFFF || d > (int64_t(1) << 20)) return PME_ERR_SHAPE;
+    if (rows > 0 && (!x || !q || !s)) return PME_ERR_NULL;
+    if (!aligned(x, xt == PME_F32 ? 4 : 2) || !aligned(q, 16) || !aligned(s, 4)) return PME_ERR_ALIGN;
+    return PME_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -424,6 +469,63 @@ pme_status pme_expanded_linear_mxfp4(const void* x, pme_dtype xt, int64_t T, int
     pme::RotateArgs ra{x, xt, T, d, ldx, d_e, b, k, qx, nullptr, nullptr, ex, nullptr, (hipStream_t)stream};
     pme::MxGemmArgs ga{qx, ex, qw, ew, T, d_e, N, y_bf16, ldy, (hipStream_t)stream};
     return run_layer(ra, ga, run_mxgemm);
+}
+
+pme_status pme_rmsnorm_quant_fp8(const void* x, pme_dtype xt, int64_t T, int64_t d, int64_t ldx, const void* residual,
+                                 int64_t ldr, void* h, int64_t ldh, const void* weight, pme_dtype wt, float eps,
+                                 uint8_t* qx, float* sx, void* stream) {
+    const pme_status st = check_quant_fp8(x, xt, T, d, ldx, qx, sx);
+    if (st != PME_OK) return st;
+    if (wt != PME_F32 && wt != PME_BF16) return PME_ERR_DTYPE;
+    if (!(eps >= 0.f) || eps > 3.4028234e38f) return PME_ERR_SHAPE;
+    if (residual && (ldr < d || ldh < d)) return PME_ERR_SHAPE;
+    if (T > 0 && (!weight || (residual == nullptr) != (h == nullptr))) return PME_ERR_NULL;
+    const size_t esz = xt == PME_F32 ? 4 : 2;
+    if (!aligned(residual, esz) || !aligned(h, esz) || !aligned(weight, wt == PME_F32 ? 4 : 2)) return PME_ERR_ALIGN;
+    if (T == 0) return PME_OK;
+    return pme::launch_rmsnorm_quant_fp8({x, xt, T, d, ldx, residual, ldr, h, ldh, weight, wt, eps, qx, sx, (hipStream_t)stream});
+}
+
+pme_status pme_quant_fp8(const void* x, pme_dtype xt, int64_t T, int64_t d, int64_t ldx, uint8_t* qx, float* sx, void* stream) {
+    const pme_status st = check_quant_fp8(x, xt, T, d, ldx, qx, sx);
+    if (st != PME_OK || T == 0) return st;
+    return pme::launch_quant_fp8({x, xt, T, d, ldx, qx, sx, (hipStream_t)stream});
+}
+
+pme_status pme_quantize_weights_fp8(const void* wt, pme_dtype wtype, int64_t N, int64_t d, int64_t ldw, uint8_t* qw, float* sw, void* stream) {
+    const pme_status st = check_quant_fp8(wt, wtype, N, d, ldw, qw, sw);
+    if (st != PME_OK || N == 0) return st;
+    return pme::launch_quantize_weights_fp8({wt, wtype, N, d, ldw, qw, sw, (hipStream_t)stream});
+}
+
+pme_status pme_fp8_gemm(const uint8_t* qx, const float* sx, const uint8_t* qw, const float* sw, int64_t T, int64_t K, int64_t N,
+                        void* y_bf16, int64_t ldy, void* stream) {
+    const pme::Fp8GemmArgs a{qx, sx, qw, sw, nullptr, nullptr, T, K, N, y_bf16, ldy, (hipStream_t)stream};
+    const pme_status st = check_fp8_gemm(a, false);
+    return st != PME_OK ? st : run_fp8_gemm(a);
+}
+
+pme_status pme_fp8_gated_gemm(const uint8_t* qx, const float* sx, const uint8_t* qg, const float* sg, const uint8_t* qu, const float* su,
+                              int64_t T, int64_t K, int64_t N, void* y_bf16, int64_t ldy, void* stream) {
+    const pme::Fp8GemmArgs a{qx, sx, qg, sg, qu, su, T, K, N, y_bf16, ldy, (hipStream_t)stream};
+    const pme_status st = check_fp8_gemm(a, true);
+    return st != PME_OK ? st : run_fp8_gemm(a);
+}
+
+pme_status pme_fp8_gemm_plan(int gated, int64_t T, int64_t K, int64_t N, char* name, size_t name_len) {
+    if (!name || name_len == 0) return PME_ERR_NULL;
+    // operands as a caller's allocations are: 256-byte aligned, never dereferenced by a dry run
+    const uint8_t* p8 = reinterpret_cast<const uint8_t*>(uintptr_t(256));
+    const float* pf = reinterpret_cast<const float*>(uintptr_t(256));
+    const char* plan = "";
+    pme::Fp8GemmArgs a{p8, pf, p8, pf, gated ? p8 : nullptr, gated ? pf : nullptr, T, K, N, const_cast<uint8_t*>(p8), N, nullptr};
+    a.dry = true;
+    a.plan = &plan;
+    pme_status st = check_fp8_gemm(a, gated != 0);
+    if (st == PME_OK && (T == 0 || N == 0)) st = PME_ERR_SHAPE;
+    if (st != PME_OK || (st = run_fp8_gemm(a)) != PME_OK) return st;
+    snprintf(name, name_len, "%s", plan);
+    return PME_OK;
 }
 
 pme_status pme_factor_order(int64_t d_e, int32_t* b, int32_t* k) {

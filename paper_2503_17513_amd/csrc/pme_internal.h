@@ -105,6 +105,50 @@ void set_rotate_tpw_override(int tpw);
 void set_mxgemm_tile_override(int id);
 int mxgemm_tile_override();
 
+// 8-bit operands with a scale for each block of 128 (e4m3 codes in whole groups of 128, fp32 scales), and the products of them.
+struct QuantArgs {
+    const void* x;       // [rows, ldx]
+    pme_dtype xt;
+    int64_t rows, d, ldx;
+    uint8_t* q;          // [rows, groups * 128]
+    float* s;            // [rows, groups], of weights [ceil(rows / 128), groups]
+    hipStream_t stream;
+};
+struct NormQuantArgs {
+    const void* x;
+    pme_dtype xt;
+    int64_t T, d, ldx;
+    const void* residual;   // null: nothing is added, h is not written
+    int64_t ldr;
+    void* h;
+    int64_t ldh;
+    const void* weight;
+    pme_dtype wt;
+    float eps;
+    uint8_t* qx;
+    float* sx;
+    hipStream_t stream;
+};
+pme_status launch_rmsnorm_quant_fp8(const NormQuantArgs& a);
+pme_status launch_quant_fp8(const QuantArgs& a);
+pme_status launch_quantize_weights_fp8(const QuantArgs& a);
+
+struct Fp8GemmArgs {
+    const uint8_t* qx;   // [T, K] e4m3
+    const float* sx;     // [T, K / 128]
+    const uint8_t* qw;   // [N, K]
+    const float* sw;     // [ceil(N / 128), K / 128]
+    const uint8_t* qu;   // gated: the second weight matrix, else null (then qw, sw are the gate's)
+    const float* su;
+    int64_t T, K, N;
+    void* y;             // bf16 [T, ldy]
+    int64_t ldy;
+    hipStream_t stream;
+    bool dry = false;    // only answer whether a kernel takes the shape: nothing is launched
+    const char** plan = nullptr;   // dry runs: receives the name of the kernel configuration that would run
+};
+pme_status launch_fp8_gemm_generic(const Fp8GemmArgs& a);
+
 // Lets `kern` be launched with up to `bytes` of dynamic LDS.  The attribute is set once per kernel and
 // device (`done` holds one bit per device and belongs to the kernel's launcher), not on every launch.
 template <class K> inline pme_status allow_dynamic_lds(K kern, int bytes, std::atomic<uint32_t>& done) {

@@ -1,0 +1,320 @@
+"""GPU parity of the 8-bit layers against the CPU oracle.
+
+Tolerances, u = 2^-24 the half step of fp32:
+  scales        amax / 448 with one correction step: 4 u; behind a norm DELTA more (below).
+  codes         a code is the e4m3 value nearest to the computed quotient: |code - quotient| <= half the step there plus the quotient's
+                own error, 8 u (the scale, its reciprocal with one correction step, one product).
+  norm          v = h pre rms w: the sum of squares is a chain of at most 8 chunks * 8 values * rounds a lane and 12 joins, each within u
+                and all terms positive, halved by the root; root, division, mean, three products: 10 u more.
+  products      exact terms; a sum of 128 in the matrix core and one of K / 128 in fp32, each addition within 2^-23 of the terms'
+                magnitudes (a truncating adder counted in): (128 + K / 128 + 4) 2^-23 sum |terms|; one rounding to bf16, 2^-8.
+  gated         |silu'| <= 1.1 and |silu(g)| <= |g|: errors of both products through them, 8 u of exp, division and product; bf16.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2503_17513_amd as pme
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+EPS = 1e-5
+
+
+@pytest.fixture(autouse=True)
+def _reset():
+    yield
+    pme.set_path(pme.PATH_AUTO)
+    pme.set_gemm_tile(0)
+
+
+def _rand(shape, seed, outliers=True, dtype=torch.bfloat16):
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal(shape)
+    if outliers:
+        x[:, rng.integers(0, shape[1], max(1, shape[1] // 100))] *= 50.0
+    return torch.from_numpy(x.astype(np.float32)).to(dtype).cuda()
+
+
+def _f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def _codes64(q):
+    return q.detach().cpu().to(torch.float32).numpy().astype(np.float64)
+
+
+def check_codes(q, s, quotient, scale, delta):
+    """Codes and scales against the oracle's quotients (before rounding) and scales."""
+    s, q = _f64(s), _codes64(q)
+    assert s.shape == scale.shape and q.shape == quotient.shape
+    rel = np.abs(s - scale) / scale
+    assert rel.max(initial=0) <= delta + 4 * U, f"scale off by {rel.max():.3e}"
+    err = np.abs(q - quotient) - oracle.e4m3_step(quotient) / 2
+    assert np.all(err <= (2 * delta + 8 * U) * np.abs(quotient)), f"code off by {err.max():.3e} more than half a step"
+    assert np.array_equal(q, oracle.e4m3_round(q))
+
+
+def norm_delta(d):
+    chunks = max(1, -(-d // 8) // 64)                # a lane's chunks, at most (rows on one wave)
+    return ((8 * chunks + 12) / 2 + 10) * U
+
+
+# ---- norm, residual, codes
+
+NORM_CASES = [
+    # T, d, type, weight type, residual
+    (1, 2048, "bf16", "bf16", True), (1, 1, "bf16", "bf16", True), (2, 7, "f32", "f32", False), (3, 127, "bf16", "f32", True),
+    (3, 128, "f32", "bf16", True), (5, 129, "bf16", "bf16", False), (4, 2000, "f32", "f32", True), (9, 4096, "bf16", "bf16", True),
+    (2, 14336, "bf16", "bf16", True), (3, 16387, "f32", "f32", True), (2, 32768, "bf16", "bf16", False), (2, 40001, "bf16", "f32", True), (1, 70000, "f32", "f32", True),
+    (1, 1 << 20, "bf16", "bf16", False), (513, 2048, "bf16", "bf16", True), (600, 1999, "bf16", "bf16", True), (700, 130, "f32", "f32", False),
+    (521, 4096, "bf16", "bf16", True), (515, 8200, "f32", "bf16", False),
+]
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.mark.parametrize("T,d,xt,wt,residual", NORM_CASES)
+def test_rmsnorm_quant(T, d, xt, wt, residual):
+    x = _rand((T, d), d + T, dtype=DT[xt])
+    w = _rand((1, d), d, outliers=False, dtype=DT[wt])[0]
+    r = _rand((T, d), d + T + 1, outliers=False, dtype=DT[xt]) if residual else None
+    if T > 2:
+        x[1] = 0
+        if residual:
+            r[1] = 0
+    out = pme.rmsnorm_quant_fp8(x, w, EPS, r)
+    torch.cuda.synchronize()
+    h = (x.float() + r.float()).to(DT[xt]) if residual else x
+    if residual:
+        assert torch.equal(out[2], h)                 # one addition and one rounding
+    quotient, scale = oracle.fp8_quotients(oracle.rmsnorm(_f64(h), _f64(w), EPS))
+    check_codes(out[0], out[1], quotient, scale, norm_delta(d))
+    if T > 2:
+        assert not _codes64(out[0])[1].any() and bool((out[1][1] == 1).all())
+
+
+def test_rmsnorm_in_place_pitches_and_odd_addresses():
+    T, d = 37, 1003
+    for xt in ("bf16", "f32"):
+        w = _rand((1, d), 5, outliers=False, dtype=DT[xt])[0]
+        big = [_rand((T, d + 30), 6 + i, dtype=DT[xt]) for i in range(3)]
+        x, r, h = big[0][:, 1:1 + d], big[1][:, 3:3 + d], big[2][:, 17:17 + d]       # odd pitches and odd first columns
+        want = (x.float() + r.float()).to(DT[xt])
+        around = [b.clone() for b in big]
+        quotient, scale = oracle.fp8_quotients(oracle.rmsnorm(_f64(want), _f64(w), EPS))
+        q, s, got = pme.rmsnorm_quant_fp8(x, w, EPS, r, h)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and got.data_ptr() == h.data_ptr()
+        check_codes(q, s, quotient, scale, norm_delta(d))
+        around[2][:, 17:17 + d] = want                # nothing beside the rows has changed
+        assert all(torch.equal(a, b) for a, b in zip(around, big))
+        for alias in (x, r):                          # the stream updated in place
+            xa, ra = x.clone(), r.clone()
+            dst = xa if alias is x else ra
+            q2, s2, h2 = pme.rmsnorm_quant_fp8(xa, w, EPS, ra, dst)
+            torch.cuda.synchronize()
+            assert torch.equal(h2, want) and torch.equal(q2.view(torch.uint8), q.view(torch.uint8)) and torch.equal(s2, s)
+
+
+@pytest.mark.parametrize("d", [256, 5000, 40000])
+def test_rmsnorm_rows_beyond_the_squares_range(d):
+    """Squares that overflow or vanish in fp32, eps of zero, zeros, values that are not finite: each row by itself."""
+    x = _rand((8, d), 3, dtype=torch.float32)
+    for i, f in enumerate((1e30, 1e-30, 1e-42, 1.0, 1e36)):
+        x[i] *= f
+    x[5] = 0
+    x[6, d // 2] = float("nan")
+    x[7, d - 1] = float("-inf")
+    w = _rand((1, d), 4, outliers=False, dtype=torch.float32)[0]
+    for eps in (0.0, 1e-30, 1e-5):
+        q, s = pme.rmsnorm_quant_fp8(x, w, eps)
+        torch.cuda.synchronize()
+        quotient, scale = oracle.fp8_quotients(oracle.rmsnorm(_f64(x[:6]), _f64(w), np.float32(eps)))
+        # behind eps = 1e-5 the row of subnormal values stays subnormal, which is not within half a step of fp32's relative rounding
+        keep = [0, 1, 2, 3, 4, 5] if eps < 1e-20 else [0, 1, 3, 4, 5]
+        check_codes(q[keep], s[keep], quotient[keep], scale[keep], norm_delta(d) + 4 * U)
+        assert bool(torch.isnan(q[6:].float()).all()) and bool(torch.isnan(s[6:]).all())
+
+
+# ---- quantizers
+
+@pytest.mark.parametrize("T,d,xt", [(1, 1, "bf16"), (3, 130, "f32"), (8, 8192, "bf16"), (5, 1999, "bf16"), (2, 40001, "f32"), (1100, 4096, "bf16"), (333, 14336, "f32"), (1, 1 << 20, "bf16")])
+def test_quant(T, d, xt):
+    x = _rand((T, d), d, dtype=DT[xt])
+    if T > 2:
+        x[1] = 0
+    q, s = pme.quant_fp8(x)
+    torch.cuda.synchronize()
+    check_codes(q, s, *oracle.fp8_quotients(_f64(x)), 0.0)
+
+
+def test_quant_extremes():
+    x = torch.zeros((7, 200), dtype=torch.float32, device="cuda")
+    x[0, 3], x[1, 150], x[2, 0], x[3, 5] = 3.4e38, 1e-40, float("inf"), float("nan")
+    x[4, 7], x[4, 8] = -1e-30, 3e-33
+    x[5, :128], x[6, 199] = 2.0, -0.0
+    q, s = pme.quant_fp8(x)
+    torch.cuda.synchronize()
+    ok = [0, 1, 4, 5, 6]
+    check_codes(q[ok], s[ok], *oracle.fp8_quotients(_f64(x[ok])), 0.0)
+    assert s[1, 1] == 2.0 ** -126
+    for row in (2, 3):
+        assert bool(torch.isnan(s[row, 0])) and bool(torch.isnan(q[row, :128].float()).all()) and s[row, 1] == 1 and not bool(q[row, 128:].float().any())
+
+
+def test_quant_pitch_and_odd_address():
+    big = _rand((19, 700), 2)
+    x = big[:, 5:5 + 301]
+    q, s = pme.quant_fp8(x)
+    torch.cuda.synchronize()
+    check_codes(q, s, *oracle.fp8_quotients(_f64(x)), 0.0)
+
+
+@pytest.mark.parametrize("N,d,xt", [(1, 1, "bf16"), (127, 130, "f32"), (128, 128, "bf16"), (129, 2000, "bf16"), (300, 1024, "f32"), (2048, 257, "bf16")])
+def test_quantize_weights(N, d, xt):
+    w = _rand((N, d + 3), N + d, dtype=DT[xt])[:, 1:1 + d]
+    if N > 256:
+        w[128:256] = 0
+    q, s = pme.quantize_weights_fp8(w)
+    torch.cuda.synchronize()
+    check_codes(q, s, *oracle.fp8_quotients_weights(_f64(w)), 0.0)
+
+
+# ---- products
+
+def _operands(T, K, N, seed, mats=1):
+    """Codes of heavy-tailed activations and Gaussian weights by the oracle's quantizer, on the device."""
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((T, K))
+    x[:, rng.integers(0, K, max(1, K // 100))] *= 50.0
+    out = []
+    for v, f in [(x, oracle.fp8_quotients)] + [(rng.standard_normal((N, K)), oracle.fp8_quotients_weights) for _ in range(mats)]:
+        quotient, s = f(v)
+        q = oracle.e4m3_round(quotient).astype(np.float32)
+        out += [torch.from_numpy(q).cuda().to(torch.float8_e4m3fn), torch.from_numpy(s.astype(np.float32)).cuda()]
+    return out
+
+
+def _products(ops):
+    qx, sx = _codes64(ops[0]), _f64(ops[1])
+    return [oracle.gemm_fp8(qx, sx, _codes64(q), _f64(s)) for q, s in zip(ops[2::2], ops[3::2])]
+
+
+def sum_bound(K):
+    return (128 + K / 128 + 4) * 2.0 ** -23
+
+
+def check_gemm(y, ops):
+    (ref, mag), = _products(ops)
+    err = np.abs(_f64(y) - ref)
+    lim = 2.0 ** -8 * np.abs(ref) + 1.01 * sum_bound(ops[0].shape[1]) * mag
+    assert np.all(err <= lim), f"product off by {np.max(err / lim):.2f} times its bound"
+
+
+def check_gated(y, ops):
+    (g, gm), (u, um) = _products(ops)
+    ref, b = oracle.gated(g, u), 1.01 * sum_bound(ops[0].shape[1])
+    lim = 2.0 ** -8 * np.abs(ref) + 1.01 * (1.1 * b * gm * np.abs(u) + np.abs(g) * b * um + 1.1 * b * gm * b * um + 8 * U * np.abs(ref))
+    err = np.abs(_f64(y) - ref)
+    assert np.all(err <= lim), f"gated product off by {np.max(err / lim):.2f} times its bound"
+
+
+PATHS = (pme.PATH_GENERIC, pme.PATH_AUTO)
+GEMM_SHAPES = [(1, 128, 1), (1, 256, 130), (3, 128, 64), (16, 384, 129), (17, 1024, 255), (33, 640, 300), (64, 2048, 256), (100, 1152, 131),
+               (130, 512, 700), (257, 1280, 513)]
+
+
+@pytest.mark.parametrize("T,K,N", GEMM_SHAPES)
+def test_fp8_gemm(T, K, N):
+    ops = _operands(T, K, N, T + K + N)
+    for path in PATHS:
+        pme.set_path(path)
+        y = pme.fp8_gemm(*ops)
+        torch.cuda.synchronize()
+        check_gemm(y, ops)
+
+
+@pytest.mark.parametrize("T,K,N", GEMM_SHAPES)
+def test_fp8_gated_gemm(T, K, N):
+    ops = _operands(T, K, N, T + K + N, mats=2)
+    for path in PATHS:
+        pme.set_path(path)
+        y = pme.fp8_gated_gemm(*ops)
+        torch.cuda.synchronize()
+        check_gated(y, ops)
+
+
+def test_products_write_their_columns_only():
+    for T, K, N in ((5, 256, 67), (150, 512, 333)):
+        ops = _operands(T, K, N, 9, mats=2)
+        for f, o in ((pme.fp8_gemm, ops[:4]), (pme.fp8_gated_gemm, ops)):
+            whole = f(*o)
+            for pad, first in ((13, 0), (16, 8), (7, 3)):
+                big = torch.full((T + 3, N + pad), 7.0, dtype=torch.bfloat16, device="cuda")
+                f(*o, big[:T, first:first + N])
+                torch.cuda.synchronize()
+                assert torch.equal(big[:T, first:first + N], whole)
+                assert bool((big[T:] == 7).all()) and bool((big[:T, :first] == 7).all()) and bool((big[:T, first + N:] == 7).all())
+
+
+def test_nan_codes_reach_their_rows_only():
+    ops = _operands(40, 384, 200, 3)
+    clean = pme.fp8_gemm(*ops)
+    ops[1][7, 1] = float("nan")                       # as the quantizers mark a block that is not finite
+    y = pme.fp8_gemm(*ops)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(y[7]).all())
+    assert torch.equal(y[:7], clean[:7]) and torch.equal(y[8:], clean[8:])
+
+
+# ---- together
+
+def _block(seed, T=70, d=640, f=704, f_e=768):
+    """A feed-forward block: norm, gated product, expanded int4 down projection."""
+    wg, wu = _rand((f, d), seed, outliers=False) / d ** 0.5, _rand((f, d), seed + 1, outliers=False) / d ** 0.5
+    wd = _rand((d, f), seed + 2, outliers=False) / f ** 0.5
+    return {"x": _rand((T, d), seed + 3), "r": _rand((T, d), seed + 4), "w": _rand((1, d), seed + 5, outliers=False)[0], "d_e": f_e,
+            "g": pme.quantize_weights_fp8(wg), "u": pme.quantize_weights_fp8(wu), "down": pme.expand_quantize_weights(wd, f_e)}
+
+
+def _run_block(b, r):
+    q, s, h = pme.rmsnorm_quant_fp8(b["x"], b["w"], EPS, r)
+    a = pme.fp8_gated_gemm(q, s, *b["g"], *b["u"])
+    return pme.expanded_linear(a, b["d_e"], *b["down"]), h, a, q, s
+
+
+def test_feed_forward_block():
+    b = _block(50)
+    y, h, a, q, s = _run_block(b, b["r"])
+    torch.cuda.synchronize()
+    assert torch.equal(h, (b["x"].float() + b["r"].float()).to(torch.bfloat16))
+    check_codes(q, s, *oracle.fp8_quotients(oracle.rmsnorm(_f64(h), _f64(b["w"]), EPS)), norm_delta(h.shape[1]))
+    check_gated(a, [q, s, *b["g"], *b["u"]])
+    ref = oracle.expanded_linear(_f64(a), b["d_e"], oracle.unpack_int4(b["down"][0].cpu().numpy()), b["down"][1].cpu().numpy())
+    # codes of the down projection that sit at a tie may differ: a flip moves an output by a weight code (at most 8) times both scales
+    step = 8 * ref["sx"][:, None] * b["down"][1].cpu().numpy()[None]
+    assert np.all(np.abs(_f64(y) - ref["y"]) <= 1e-2 * np.abs(ref["y"]) + 2 * step)
+
+
+def test_block_on_another_stream_and_replayed():
+    """The block captured into a graph: every replay, with the program's own work between, equals the eager run on the same inputs."""
+    b = _block(80, T=33)
+    want = [t.clone() for t in _run_block(b, b["r"])]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = _run_block(b, b["r"])
+    side.synchronize()
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(want, got))
+    graph = torch.cuda.CUDAGraph()
+    r = b["r"].clone()
+    with torch.cuda.graph(graph):
+        out = _run_block(b, r)
+    for k in range(4):
+        r.copy_(b["r"] * (k + 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = _run_block(b, b["r"] * (k + 1))
+        torch.cuda.synchronize()
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(eager, out))
