@@ -5,9 +5,13 @@
 #include "gemm_tile.h"
 
 #include <algorithm>
+#include <cstdio>
+#include <string>
 
 namespace pme {
 namespace {
+
+typedef __attribute__((ext_vector_type(8))) int i32x8;
 
 __device__ __forceinline__ float silu(float v) { return v / (1.f + expf(-v)); }
 
@@ -43,7 +47,276 @@ k_fp8_gemm_generic(const uint8_t* __restrict__ qx, const float* __restrict__ sx,
     }
 }
 
+
+// As dma16, from a buffer: dwords beyond its end arrive as zeros.
+__device__ __forceinline__ void dma16_buffer(u32x4 rsrc, uint32_t voff, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "s"(lds_base) : "memory");
+}
+// Buffer descriptor of `bytes` bytes at p.
+__device__ __forceinline__ u32x4 buffer_of(const void* p, uint32_t bytes) {
+    const uint64_t a = (uint64_t)(uintptr_t)p;
+    return u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xFFFFu, bytes, 0x00027000u};
+}
+
+__device__ __forceinline__ int swz16(int r) { return (r >> 1) & 7; }
+
+struct Fp8TileArgs {
+    const uint8_t* qx;
+    const float* sx;
+    const uint8_t* qw;
+    const float* sw;
+    const uint8_t* qu;
+    const float* su;
+    int T, N, K;
+    uint16_t* y;
+    int64_t ldo;
+    int tiles_m, tiles_n, xcd_gm, vec_store;
+};
+
+constexpr int fp8_stage(int bm, int bn, int ks) { return ks * (bm + bn) * 128; }
+constexpr int fp8_scale_blocks(int bm, bool gated) { return (bm + 63) / 64 + (gated ? 2 : 1); }
+constexpr int fp8_lds(int bm, int bn, int ks, int nstage, bool gated) { return nstage * fp8_stage(bm, bn, ks) + 2 * 1024 * fp8_scale_blocks(bm, gated); }
+
+template <int BM, int BN, int WGM, int WGN, int KS, int NSTAGE, bool GATED>
+__global__ void __launch_bounds__(64 * WGM * WGN * KS)
+k_fp8_gemm(const Fp8TileArgs p) {
+    constexpr int NWW = WGM * WGN;                               // waves of a slice of K
+    constexpr int WM = BM / WGM, WN = BN / WGN, FM = WM / 16, FN = WN / 16;
+    constexpr int BO = GATED ? BN / 2 : BN, WO = GATED ? WN / 2 : WN, FO = WO / 16;      // output channels of the tile, of a wave, in blocks
+    constexpr int ROWS = BM + BN, STAGE = fp8_stage(BM, BN, KS), SLICE = ROWS * 128;
+    constexpr int CH = ROWS / 8 / NWW;                           // DMA instructions per wave and stage
+    constexpr int XB = (BM + 63) / 64, SBLKS = fp8_scale_blocks(BM, GATED), GROUP = SBLKS * 1024, SCALES = NSTAGE * STAGE;
+    constexpr int GS = 4 / KS;                                   // stages of a group of scales
+    static_assert(KS == 1 || KS == 2 || KS == 4, "a group of scales is whole stages");
+    static_assert(ROWS / 8 % NWW == 0 && BM % 8 == 0 && BO % 8 == 0, "whole DMA blocks for every wave, none across operands");
+    static_assert(128 % WO == 0 && WM % 16 == 0 && WO % 16 == 0, "a wave's channels lie in one block of scales");
+    static_assert(BO <= 128 || BO == 256, "a tile has the scales of one or two blocks of channels");
+
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int w = wave % NWW, ks = wave / NWW, wm = w / WGN, wn = w % WGN;
+    int tm, tn;
+    xcd_tile((int)blockIdx.x, p.tiles_m, p.tiles_n, p.xcd_gm, tm, tn);
+    const int m0 = tm * BM, n0 = tn * BO, groups = p.K / 128, KT = (groups + KS - 1) / KS;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(PME_AS3 unsigned char*)smem;
+
+    // DMA of codes: block blk is rows 8 blk .. 8 blk + 7 of the wave's slice (tokens, channels, gated: the second matrix's channels);
+    // lane L fills chunk position L % 8 of row L / 8, which holds chunk (L % 8) ^ swz
+    uint32_t voff[CH];
+#pragma unroll
+    for (int q = 0; q < CH; ++q) {
+        const int r = 8 * (w + NWW * q) + (lane >> 3), b = r - BM;
+        const int row = r < BM ? min(m0 + r, p.T - 1) : min(n0 + (b < BO ? b : b - BO), p.N - 1);
+        voff[q] = (uint32_t)row * (uint32_t)p.K + (uint32_t)(((lane & 7) ^ swz16(r)) << 4);
+    }
+    auto issue_codes = [&](int stage, int kt, int q) {           // K block beyond the last: the last again, which nobody reads
+        const int blk = w + NWW * q, kb = min(kt * KS + ks, groups - 1);
+        const uint8_t* base = blk < BM / 8 ? p.qx : (GATED && blk >= (BM + BO) / 8) ? p.qu : p.qw;
+        dma16(base + (int64_t)kb * 128, voff[q], __builtin_amdgcn_readfirstlane(lds0 + stage * STAGE + ks * SLICE + blk * 1024));
+    };
+    // of scales: sixteen bytes, four K blocks, of a token or of a block of channels; group g goes to place g & 1
+    const uint32_t rowb = (uint32_t)groups * 4;
+    const u32x4 sx_buf = buffer_of(p.sx, (uint32_t)p.T * rowb), sw_buf = buffer_of(p.sw, (uint32_t)((p.N + 127) / 128) * rowb);
+    const u32x4 su_buf = buffer_of(GATED ? p.su : p.sw, (uint32_t)((p.N + 127) / 128) * rowb);
+    auto issue_scales = [&](int g) {
+#pragma unroll
+        for (int s = 0; s < SBLKS; ++s) {
+            if (s % (NWW * KS) != wave) continue;
+            const int row = s < XB ? min(m0 + min(64 * s + lane, BM - 1), p.T - 1) : min(n0 / 128 + min(lane, 1), (p.N - 1) / 128);
+            dma16_buffer(s < XB ? sx_buf : s == XB ? sw_buf : su_buf, (uint32_t)row * rowb + 16 * (uint32_t)g,
+                         __builtin_amdgcn_readfirstlane(lds0 + SCALES + (g & 1) * GROUP + s * 1024));
+        }
+    };
+
+    f32x4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    const int r16 = lane & 15, kg = lane >> 4;
+    // chunk 4 q + kg of a row is at position (kg ^ swz) ^ 4 q; rows 16 apart share their swizzle
+    const int aoff = (wm * WM + r16) * 128 + ((kg ^ swz16(r16)) << 4), boff = (BM + wn * WO + r16) * 128 + ((kg ^ swz16(r16)) << 4);
+    const int nb = (n0 + wn * WO) / 128 - n0 / 128;              // the wave's block of channels within the tile
+    auto frag = [&](const unsigned char* at) {
+        const u32x4 lo = *reinterpret_cast<const u32x4*>(at), hi = *reinterpret_cast<const u32x4*>(smem + ((at - smem) ^ 64));
+        return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    };
+    auto load_a = [&](int slice, int i) { return frag(smem + slice + aoff + 16 * 128 * i); };
+    auto load_b = [&](int slice, int j) { return frag(smem + slice + boff + 128 * (GATED && j >= FO ? BO + 16 * (j - FO) : 16 * j)); };
+
+    // prologue
+    issue_scales(0);
+    issue_scales(1);
+#pragma unroll
+    for (int st = 0; st < NSTAGE - 1; ++st)
+#pragma unroll
+        for (int q = 0; q < CH; ++q) issue_codes(st, st, q);
+    int cur = 0;
+    for (int kt = 0; kt < KT; ++kt) {
+        // this wave's DMA of K step kt has landed, then every wave's; every wave has left the stage of step kt - 1
+        wait_vm<(NSTAGE - 2) * CH>();
+        lds_barrier();
+        const int fill = cur == 0 ? NSTAGE - 1 : cur - 1;
+        if (kt > 0 && kt % GS == 0) issue_scales(kt / GS + 1);
+        const int slice = cur * STAGE + ks * SLICE, kb = kt * KS + ks;
+        if (kb < groups) {
+            const unsigned char* sc = smem + SCALES + ((kt / GS) & 1) * GROUP + 4 * (kb & 3);
+            float pw[FM], pu[FM];
+            const float swv = *reinterpret_cast<const float*>(sc + XB * 1024 + 16 * nb);
+            const float suv = GATED ? *reinterpret_cast<const float*>(sc + (XB + 1) * 1024 + 16 * nb) : 0.f;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const float v = *reinterpret_cast<const float*>(sc + 16 * (wm * WM + 16 * i + r16));
+                pw[i] = v * swv;
+                pu[i] = v * suv;
+            }
+            i32x8 a[FM], b[2];
+#pragma unroll
+            for (int i = 0; i < FM; ++i) a[i] = load_a(slice, i);
+            b[0] = load_b(slice, 0);
+            f32x4 t[2][FM];
+            static_for<FN>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                if constexpr (j + 1 < FN) b[(j + 1) & 1] = load_b(slice, j + 1);
+                static_for<CH>([&](auto qc) {
+                    if constexpr (decltype(qc)::value * FN / CH == j) issue_codes(fill, kt + NSTAGE - 1, decltype(qc)::value);
+                });
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    t[j & 1][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j & 1], a[i], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+                    if constexpr (j > 0) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][j - 1][e] = fmaf(t[(j - 1) & 1][i][e], GATED && j - 1 >= FO ? pu[i] : pw[i], acc[i][j - 1][e]);
+                    }
+                }
+            });
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][FN - 1][e] = fmaf(t[(FN - 1) & 1][i][e], GATED ? pu[i] : pw[i], acc[i][FN - 1][e]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < CH; ++q) issue_codes(fill, kt + NSTAGE - 1, q);
+        }
+        cur = cur == NSTAGE - 1 ? 0 : cur + 1;
+    }
+    wait_vm<0>();
+    lds_barrier();
+
+    // ---- the slices of K are added in LDS: slice i % KS finishes the 16 tokens of group i
+    if constexpr (KS > 1) {
+        f32x4* part = reinterpret_cast<f32x4*>(smem);
+        static_assert(NWW * FM * KS * FN * 1024 <= NSTAGE * STAGE, "the partial sums go through the stages");
+        auto at = [&](int i, int slice, int j) { return part + ((((w * FM + i) * KS + slice) * FN + j) * 64 + lane); };
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+            if (i % KS != ks) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j) *at(i, ks, j) = acc[i][j];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+            if (i % KS == ks) {
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    if (s != i % KS) {
+#pragma unroll
+                        for (int j = 0; j < FN; ++j) acc[i][j] += *at(i, s, j);
+                    }
+            }
+        __syncthreads();
+    }
+
+    // ---- epilogue: element e of block (i, j) is token m0 + wm WM + 16 i + r16, channel n0 + wn WO + 16 j + 4 kg + e.  The 16 tokens of a
+    // group go through LDS (private to the wave) into 16-byte pieces of rows.
+    constexpr int SLAB = 16 * WO * 2;
+    static_assert(NWW * KS * SLAB <= NSTAGE * STAGE, "the slabs go through the stages");
+    unsigned char* slab = smem + wave * SLAB;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        if (i % KS != ks) continue;
+#pragma unroll
+        for (int j = 0; j < FO; ++j) {
+            f32x4 v = acc[i][j];
+            if constexpr (GATED) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = silu(v[e]) * acc[i][j + FO][e];
+            }
+            *reinterpret_cast<u32x2*>(slab + r16 * (WO * 2) + (16 * j + 4 * kg) * 2) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const int tbase = m0 + wm * WM + 16 * i, nbase = n0 + wn * WO;
+        if (p.vec_store) {
+            constexpr int CPS = WO / 8;
+#pragma unroll
+            for (int c = lane; c < 16 * CPS; c += 64) {
+                const int row = c / CPS, col = (c % CPS) * 8;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(slab + row * (WO * 2) + col * 2);
+                if (tbase + row < p.T && nbase + col < p.N) *reinterpret_cast<u32x4*>(p.y + (int64_t)(tbase + row) * p.ldo + nbase + col) = v;
+            }
+        } else {
+            for (int c = lane; c < 16 * WO; c += 64) {
+                const int row = c / WO, col = c % WO;
+                if (tbase + row < p.T && nbase + col < p.N)
+                    p.y[(int64_t)(tbase + row) * p.ldo + nbase + col] = *reinterpret_cast<const uint16_t*>(slab + row * (WO * 2) + col * 2);
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+}
+
+template <int BM, int BN, int WGM, int WGN, int KS, int NSTAGE, bool GATED> pme_status launch_tile(const Fp8GemmArgs& a) {
+    if (a.dry) {
+        if (a.plan) {
+            // the instantiation's name as a profiler prints it
+            static const std::string name = [] {
+                char buf[96];
+                snprintf(buf, sizeof buf, "k_fp8_gemm<%d, %d, %d, %d, %d, %d, %s>", BM, BN, WGM, WGN, KS, NSTAGE, GATED ? "true" : "false");
+                return std::string(buf);
+            }();
+            *a.plan = name.c_str();
+        }
+        return PME_OK;
+    }
+    constexpr int BO = GATED ? BN / 2 : BN;
+    constexpr int lds = fp8_lds(BM, BN, KS, NSTAGE, GATED);
+    static_assert(lds <= 160 * 1024, "LDS of a compute unit");
+    const int tiles_m = (int)((a.T + BM - 1) / BM), tiles_n = (int)((a.N + BO - 1) / BO);
+    auto kern = k_fp8_gemm<BM, BN, WGM, WGN, KS, NSTAGE, GATED>;
+    static std::atomic<uint32_t> done;
+    if (allow_dynamic_lds(kern, lds, done) != PME_OK) return PME_ERR_HIP;
+    const int vec = (a.N % 8 == 0 && a.ldy % 8 == 0 && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0) ? 1 : 0;
+    const Fp8TileArgs p{a.qx, a.sx, a.qw, a.sw, a.qu, a.su, (int)a.T, (int)a.N, (int)a.K, static_cast<uint16_t*>(a.y), a.ldy,
+                        tiles_m, tiles_n, xcd_grid_m(tiles_m, tiles_n, BM, BN), vec};
+    hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * WGM * WGN * KS), lds, a.stream, p);
+    return hip_status(hipGetLastError());
+}
+
+int g_fp8_tile_override = 0;
+
+template <bool GATED> pme_status launch_one(const Fp8GemmArgs& a, int id) {
+    switch (id) {
+        case 1: return launch_tile<256, 256, 4, 2, 1, 2, GATED>(a);
+        case 2: return launch_tile<128, 256, 2, 4, 1, 3, GATED>(a);
+        case 3: return launch_tile<128, 128, 2, 2, 2, 2, GATED>(a);
+        case 4: return launch_tile<64, 128, 2, 2, 2, 2, GATED>(a);
+        case 5: return launch_tile<64, 64, 2, 2, 2, 3, GATED>(a);
+        case 6: return launch_tile<32, 64, 1, 2, 4, 3, GATED>(a);
+        case 7: return launch_tile<32, 32, 1, 1, 4, 3, GATED>(a);
+    }
+    return PME_ERR_UNSUPPORTED_PATH;
+}
+
 }  // namespace
+
+void set_fp8_tile_override(int id) { g_fp8_tile_override = id; }
+
+pme_status launch_fp8_gemm_mfma(const Fp8GemmArgs& a) {
+    const int id = g_fp8_tile_override ? g_fp8_tile_override : a.T > 128 ? 1 : a.T > 64 ? 3 : a.T > 32 ? 5 : 7;
+    return a.qu ? launch_one<true>(a, id) : launch_one<false>(a, id);
+}
 
 pme_status launch_fp8_gemm_generic(const Fp8GemmArgs& a) {
     if (a.dry) {

@@ -195,7 +195,14 @@ pme_status check_fp8_gemm(const pme::Fp8GemmArgs& a, bool gated) {
     return PME_OK;
 }
 
-pme_status run_fp8_gemm_slice(const pme::Fp8GemmArgs& a) { return pme::launch_fp8_gemm_generic(a); }
+pme_status run_fp8_gemm_slice(const pme::Fp8GemmArgs& a) {
+    const int path = g_path.load();
+    if (path != PME_PATH_GENERIC) {
+        const pme_status s = pme::launch_fp8_gemm_mfma(a);
+        if (s != PME_ERR_UNSUPPORTED_PATH || path == PME_PATH_MFMA) return s;
+    }
+    return pme::launch_fp8_gemm_generic(a);
+}
 
 pme_status run_fp8_gemm(const pme::Fp8GemmArgs& a) {
     if (a.T == 0 || a.N == 0) return PME_OK;
@@ -589,9 +596,13 @@ pme_status pme_probe_mfma(int kind, int32_t* out, size_t out_elems, int iters, d
 }
 
 void pme_set_gemm_tile(int id) {
+    if (id >= 200) { pme::set_fp8_tile_override(id - 200); return; }
     if (id >= 100) { pme::set_mxgemm_tile_override(id - 100); return; }
     pme::set_gemm_tile_override(id);
-    if (id == 0) pme::set_mxgemm_tile_override(0);
+    if (id == 0) {
+        pme::set_mxgemm_tile_override(0);
+        pme::set_fp8_tile_override(0);
+    }
 }
 void pme_set_path(pme_path p) { g_path.store((int)p); }
 pme_path pme_get_path(void) { return (pme_path)g_path.load(); }

@@ -148,6 +148,8 @@ struct Fp8GemmArgs {
     const char** plan = nullptr;   // dry runs: receives the name of the kernel configuration that would run
 };
 pme_status launch_fp8_gemm_generic(const Fp8GemmArgs& a);
+pme_status launch_fp8_gemm_mfma(const Fp8GemmArgs& a);
+void set_fp8_tile_override(int id);
 
 // Lets `kern` be launched with up to `bytes` of dynamic LDS.  The attribute is set once per kernel and
 // device (`done` holds one bit per device and belongs to the kernel's launcher), not on every launch.

@@ -6,8 +6,11 @@ Tolerances, u = 2^-24 the half step of fp32:
                 own error, 8 u (the scale, its reciprocal with one correction step, one product).
   norm          v = h pre rms w: the sum of squares is a chain of at most 8 chunks * 8 values * rounds a lane and 12 joins, each within u
                 and all terms positive, halved by the root; root, division, mean, three products: 10 u more.
-  products      exact terms; a sum of 128 in the matrix core and one of K / 128 in fp32, each addition within 2^-23 of the terms'
-                magnitudes (a truncating adder counted in): (128 + K / 128 + 4) 2^-23 sum |terms|; one rounding to bf16, 2^-8.
+  products      exact terms.  The matrix instruction adds the products of eight consecutive codes on the grid of 13 bits below the
+                largest exponent among them (test_matrix_instruction_adds_runs_of_eight_on_a_grid pins it): seven of them lose less than a
+                step each, 7 * 2^-13 max |term| of every run, counted for its products alone; further additions, 16 in the instruction and
+                one of K / 128 in fp32, each within 2^-23 of the terms' magnitudes (a truncating adder counted in; 128 for the plain kernel,
+                which adds one product at a time): (128 + K / 128 + 4) 2^-23 sum |terms|; one rounding to bf16, 2^-8.
   gated         |silu'| <= 1.1 and |silu(g)| <= |g|: errors of both products through them, 8 u of exp, division and product; bf16.
 """
 import numpy as np
@@ -201,23 +204,52 @@ def _products(ops):
     return [oracle.gemm_fp8(qx, sx, _codes64(q), _f64(s)) for q, s in zip(ops[2::2], ops[3::2])]
 
 
-def sum_bound(K):
-    return (128 + K / 128 + 4) * 2.0 ** -23
+def _sum_errors(ops, mags):
+    """Bounds on the errors of the sums behind `mags`: additions in fp32, and the grid of the matrix instruction."""
+    K = ops[0].shape[1]
+    out = []
+    x = np.abs(_codes64(ops[0]) * np.repeat(_f64(ops[1]), 128, axis=1))
+    for (q, s), mag in zip(zip(ops[2::2], ops[3::2]), mags):
+        w = np.abs(_codes64(q) * np.repeat(np.repeat(_f64(s), 128, axis=0)[: len(q)], 128, axis=1))
+        runs = np.zeros_like(mag)
+        for k in range(0, K, 8):
+            best = np.zeros_like(mag)
+            for e in range(k, k + 8):
+                np.maximum(best, np.outer(x[:, e], w[:, e]), out=best)
+            runs += best
+        out.append(1.01 * ((128 + K / 128 + 4) * 2.0 ** -23 * mag + 7 * 2.0 ** -13 * runs))
+    return out
 
 
 def check_gemm(y, ops):
     (ref, mag), = _products(ops)
     err = np.abs(_f64(y) - ref)
-    lim = 2.0 ** -8 * np.abs(ref) + 1.01 * sum_bound(ops[0].shape[1]) * mag
+    lim = 2.0 ** -8 * np.abs(ref) + 1.01 * _sum_errors(ops, [mag])[0]
     assert np.all(err <= lim), f"product off by {np.max(err / lim):.2f} times its bound"
 
 
 def check_gated(y, ops):
     (g, gm), (u, um) = _products(ops)
-    ref, b = oracle.gated(g, u), 1.01 * sum_bound(ops[0].shape[1])
-    lim = 2.0 ** -8 * np.abs(ref) + 1.01 * (1.1 * b * gm * np.abs(u) + np.abs(g) * b * um + 1.1 * b * gm * b * um + 8 * U * np.abs(ref))
+    ref = oracle.gated(g, u)
+    dg, du = _sum_errors(ops, [gm, um])
+    lim = 2.0 ** -8 * np.abs(ref) + 1.01 * (1.1 * dg * np.abs(u) + np.abs(g) * du + 1.1 * dg * du + 8 * U * np.abs(ref))
     err = np.abs(_f64(y) - ref)
     assert np.all(err <= lim), f"gated product off by {np.max(err / lim):.2f} times its bound"
+
+
+def test_matrix_instruction_adds_runs_of_eight_on_a_grid():
+    """448 * 256 in one run of eight products and its negative in the next: what is left of a small product in the first run is what lies
+    on the grid, 13 bits below the exponent 16 of the large one; in a run of its own all of it is left."""
+    x, w = torch.zeros((1, 128), device="cuda"), torch.zeros((1, 128), device="cuda")
+    x[0, 0], x[0, 8], w[0, 0], w[0, 8] = 448.0, -448.0, 256.0, 256.0
+    one = torch.ones((1, 1), device="cuda")
+    pme.set_path(pme.PATH_MFMA)
+    for at, small, left in ((5, 8.0, 8.0), (7, 24.0, 24.0), (5, 4.0, 0.0), (3, -8.0, -8.0), (16, 4.0, 4.0), (127, 0.25, 0.25)):
+        xs, ws = x.clone(), w.clone()
+        xs[0, at], ws[0, at] = small, 1.0
+        y = pme.fp8_gemm(xs.to(torch.float8_e4m3fn), one, ws.to(torch.float8_e4m3fn), one)
+        torch.cuda.synchronize()
+        assert float(y) == left, (at, small)
 
 
 PATHS = (pme.PATH_GENERIC, pme.PATH_AUTO)
@@ -243,6 +275,23 @@ def test_fp8_gated_gemm(T, K, N):
         y = pme.fp8_gated_gemm(*ops)
         torch.cuda.synchronize()
         check_gated(y, ops)
+
+
+# every tile, forced: one K block, K blocks that fill neither a stage nor a group of four scales, several tiles with ragged ends
+TILES = range(201, 208)
+TILE_SHAPES = [(1, 128, 16), (40, 384, 72), (300, 640, 530), (257, 1152, 385), (96, 2432, 128)]
+
+
+@pytest.mark.parametrize("T,K,N", TILE_SHAPES)
+@pytest.mark.parametrize("tile", TILES)
+def test_fp8_tiles(tile, T, K, N):
+    ops = _operands(T, K, N, tile + T + K + N, mats=2)
+    pme.set_path(pme.PATH_MFMA)
+    pme.set_gemm_tile(tile)
+    y, z = pme.fp8_gemm(*ops[:4]), pme.fp8_gated_gemm(*ops)
+    torch.cuda.synchronize()
+    check_gemm(y, ops[:4])
+    check_gated(z, ops)
 
 
 def test_products_write_their_columns_only():
