@@ -137,69 +137,91 @@ k_fp8_gemm(const Fp8TileArgs p) {
     const int r16 = lane & 15, kg = lane >> 4;
     // chunk 4 q + kg of a row is at position (kg ^ swz) ^ 4 q; rows 16 apart share their swizzle
     const int aoff = (wm * WM + r16) * 128 + ((kg ^ swz16(r16)) << 4), boff = (BM + wn * WO + r16) * 128 + ((kg ^ swz16(r16)) << 4);
-    const int nb = (n0 + wn * WO) / 128 - n0 / 128;              // the wave's block of channels within the tile
-    auto frag = [&](const unsigned char* at) {
-        const u32x4 lo = *reinterpret_cast<const u32x4*>(at), hi = *reinterpret_cast<const u32x4*>(smem + ((at - smem) ^ 64));
-        return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    const int soff = 16 * (wm * WM + r16), swoff = XB * 1024 + 16 * ((n0 + wn * WO) / 128 - n0 / 128);      // the wave's block of channels within the tile
+    auto frag = [&](const unsigned char* lo, const unsigned char* hi) {
+        const u32x4 a = *reinterpret_cast<const u32x4*>(lo), b = *reinterpret_cast<const u32x4*>(hi);
+        return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
     };
-    auto load_a = [&](int slice, int i) { return frag(smem + slice + aoff + 16 * 128 * i); };
-    auto load_b = [&](int slice, int j) { return frag(smem + slice + boff + 128 * (GATED && j >= FO ? BO + 16 * (j - FO) : 16 * j)); };
+    // of the K step in stage st: byte offsets of the slice's codes, of its scales
+    auto codes_of = [&](int stage) { return stage * STAGE + ks * SLICE; };
+    auto scales_of = [&](int kt) { return SCALES + ((kt / GS) & 1) * GROUP + 4 * ((kt * KS + ks) & 3); };
+    auto load_a = [&](int at, int i) { return frag(smem + (at + aoff) + 2048 * i, smem + (at + (aoff ^ 64)) + 2048 * i); };
+    auto load_b = [&](int at, int j) {
+        const int row = 128 * (GATED && j >= FO ? BO + 16 * (j - FO) : 16 * j);
+        return frag(smem + (at + boff) + row, smem + (at + (boff ^ 64)) + row);
+    };
+    i32x8 a[FM], b[2];
+    float sx[FM], sw, su, pw[FM], pu[FM];
+    auto load_sx = [&](int at, int i) { sx[i] = *reinterpret_cast<const float*>(smem + (at + soff) + 256 * i); };
+    auto load_sw = [&](int at) {
+        sw = *reinterpret_cast<const float*>(smem + (at + swoff));
+        if constexpr (GATED) su = *reinterpret_cast<const float*>(smem + (at + swoff) + 1024);
+    };
 
     // prologue
     issue_scales(0);
     issue_scales(1);
 #pragma unroll
-    for (int st = 0; st < NSTAGE - 1; ++st)
+    for (int st = 0; st < NSTAGE; ++st)
 #pragma unroll
-        for (int q = 0; q < CH; ++q) issue_codes(st, st, q);
+        for (int q = 0; q < (st == NSTAGE - 1 ? 0 : CH); ++q) issue_codes(st, st, q);
+    wait_vm<(NSTAGE - 2) * CH>();
+    lds_barrier();
+    load_sw(scales_of(0));
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+        a[i] = load_a(codes_of(0), i);
+        load_sx(scales_of(0), i);
+    }
+    b[0] = load_b(codes_of(0), 0);
+    static_assert(FN % 2 == 0, "the next step's first fragment goes to the same place");
     int cur = 0;
     for (int kt = 0; kt < KT; ++kt) {
-        // this wave's DMA of K step kt has landed, then every wave's; every wave has left the stage of step kt - 1
-        wait_vm<(NSTAGE - 2) * CH>();
-        lds_barrier();
-        const int fill = cur == 0 ? NSTAGE - 1 : cur - 1;
-        if (kt > 0 && kt % GS == 0) issue_scales(kt / GS + 1);
-        const int slice = cur * STAGE + ks * SLICE, kb = kt * KS + ks;
-        if (kb < groups) {
-            const unsigned char* sc = smem + SCALES + ((kt / GS) & 1) * GROUP + 4 * (kb & 3);
-            float pw[FM], pu[FM];
-            const float swv = *reinterpret_cast<const float*>(sc + XB * 1024 + 16 * nb);
-            const float suv = GATED ? *reinterpret_cast<const float*>(sc + (XB + 1) * 1024 + 16 * nb) : 0.f;
+        const int nxt = cur == NSTAGE - 1 ? 0 : cur + 1, prv = cur == 0 ? NSTAGE - 1 : cur - 1;
+        if (kt > 0 && kt % GS == 0) issue_scales(kt / GS + 1);       // into the place that the last step has left
+        // a slice of K that has no block left in the last step works on its last block again, with a scale of zero
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const float v = *reinterpret_cast<const float*>(sc + 16 * (wm * WM + 16 * i + r16));
-                pw[i] = v * swv;
-                pu[i] = v * suv;
-            }
-            i32x8 a[FM], b[2];
-#pragma unroll
-            for (int i = 0; i < FM; ++i) a[i] = load_a(slice, i);
-            b[0] = load_b(slice, 0);
-            f32x4 t[2][FM];
-            static_for<FN>([&](auto jc) {
-                constexpr int j = decltype(jc)::value;
-                if constexpr (j + 1 < FN) b[(j + 1) & 1] = load_b(slice, j + 1);
-                static_for<CH>([&](auto qc) {
-                    if constexpr (decltype(qc)::value * FN / CH == j) issue_codes(fill, kt + NSTAGE - 1, decltype(qc)::value);
-                });
-#pragma unroll
-                for (int i = 0; i < FM; ++i) {
-                    t[j & 1][i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j & 1], a[i], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-                    if constexpr (j > 0) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j - 1][e] = fmaf(t[(j - 1) & 1][i][e], GATED && j - 1 >= FO ? pu[i] : pw[i], acc[i][j - 1][e]);
-                    }
-                }
-            });
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][FN - 1][e] = fmaf(t[(FN - 1) & 1][i][e], GATED ? pu[i] : pw[i], acc[i][FN - 1][e]);
-        } else {
-#pragma unroll
-            for (int q = 0; q < CH; ++q) issue_codes(fill, kt + NSTAGE - 1, q);
+        for (int i = 0; i < FM; ++i) {
+            const float v = KS == 1 || kt * KS + ks < groups ? sx[i] : 0.f;
+            pw[i] = v * sw;
+            pu[i] = GATED ? v * su : 0.f;
         }
-        cur = cur == NSTAGE - 1 ? 0 : cur + 1;
+        f32x4 t[4];
+        auto add = [&](auto mc) {
+            constexpr int m = decltype(mc)::value, i = m % FM, j = m / FM;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[m & 3][e], GATED && j >= FO ? pu[i] : pw[i], acc[i][j][e]);
+        };
+        static_for<FN>([&](auto jc) {
+            constexpr int j = decltype(jc)::value;
+            if constexpr (j + 1 < FN) {
+                b[(j + 1) & 1] = load_b(codes_of(cur), j + 1);
+                static_for<CH>([&](auto qc) {
+                    if constexpr (decltype(qc)::value * (FN - 1) / CH == j) issue_codes(prv, kt + NSTAGE - 1, decltype(qc)::value);
+                });
+            } else {
+                // every operand of this step is in registers: the next step's have landed, by this wave's DMA and then by every wave's
+                wait_vm<(NSTAGE - 2) * CH>();
+                lds_barrier();
+                b[0] = load_b(codes_of(nxt), 0);
+                load_sw(scales_of(kt + 1));
+            }
+            static_for<FM>([&](auto ic) {
+                constexpr int i = decltype(ic)::value, m = j * FM + i;
+                t[m & 3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j & 1], a[i], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+                if constexpr (j == FN - 1) {
+                    a[i] = load_a(codes_of(nxt), i);
+                    load_sx(scales_of(kt + 1), i);
+                }
+                if constexpr (m >= 3) add(std::integral_constant<int, m - 3>{});
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+        static_for<3>([&](auto rc) {
+            constexpr int m = FM * FN - 3 + decltype(rc)::value;
+            if constexpr (m >= 0) add(std::integral_constant<int, m>{});
+        });
+        cur = nxt;
     }
     wait_vm<0>();
     lds_barrier();
