@@ -2,7 +2,7 @@
 //
 //   p[t][n] = sum_g sx[t][g] sw[n / 128][g] sum_{k in group g} qx[t][k] qw[n][k],   y = bf16(p),
 //   gated:  y = bf16( p_g / (1 + e^-p_g) p_u )  of two weight matrices.
-#include "gemm_tile.h"
+#include "gemm_fp8.h"
 
 #include <algorithm>
 #include <cstdio>
@@ -10,10 +10,6 @@
 
 namespace pme {
 namespace {
-
-typedef __attribute__((ext_vector_type(8))) int i32x8;
-
-__device__ __forceinline__ float silu(float v) { return v / (1.f + expf(-v)); }
 
 // Plain-ALU kernel, one thread per output: every shape, and the cross-check of the matrix-core kernels.
 template <bool GATED>
@@ -48,31 +44,6 @@ k_fp8_gemm_generic(const uint8_t* __restrict__ qx, const float* __restrict__ sx,
 }
 
 
-// As dma16, from a buffer: dwords beyond its end arrive as zeros.
-__device__ __forceinline__ void dma16_buffer(u32x4 rsrc, uint32_t voff, uint32_t lds_base) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "s"(lds_base) : "memory");
-}
-// Buffer descriptor of `bytes` bytes at p.
-__device__ __forceinline__ u32x4 buffer_of(const void* p, uint32_t bytes) {
-    const uint64_t a = (uint64_t)(uintptr_t)p;
-    return u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xFFFFu, bytes, 0x00027000u};
-}
-
-__device__ __forceinline__ int swz16(int r) { return (r >> 1) & 7; }
-
-struct Fp8TileArgs {
-    const uint8_t* qx;
-    const float* sx;
-    const uint8_t* qw;
-    const float* sw;
-    const uint8_t* qu;
-    const float* su;
-    int T, N, K;
-    uint16_t* y;
-    int64_t ldo;
-    int tiles_m, tiles_n, xcd_gm, vec_store;
-};
-
 constexpr int fp8_stage(int bm, int bn, int ks) { return ks * (bm + bn) * 128; }
 constexpr int fp8_scale_blocks(int bm, bool gated) { return (bm + 63) / 64 + (gated ? 2 : 1); }
 constexpr int fp8_lds(int bm, int bn, int ks, int nstage, bool gated) { return nstage * fp8_stage(bm, bn, ks) + 2 * 1024 * fp8_scale_blocks(bm, gated); }
@@ -87,6 +58,7 @@ k_fp8_gemm(const Fp8TileArgs p) {
     constexpr int CH = ROWS / 8 / NWW;                           // DMA instructions per wave and stage
     constexpr int XB = (BM + 63) / 64, SBLKS = fp8_scale_blocks(BM, GATED), GROUP = SBLKS * 1024, SCALES = NSTAGE * STAGE;
     constexpr int GS = 4 / KS;                                   // stages of a group of scales
+    constexpr int DJ = FN - 1 < 2 ? FN - 1 : 2;                  // regions of the K step that carry the DMA of a later one
     static_assert(KS == 1 || KS == 2 || KS == 4, "a group of scales is whole stages");
     static_assert(ROWS / 8 % NWW == 0 && BM % 8 == 0 && BO % 8 == 0, "whole DMA blocks for every wave, none across operands");
     static_assert(128 % WO == 0 && WM % 16 == 0 && WO % 16 == 0, "a wave's channels lie in one block of scales");
@@ -197,7 +169,7 @@ k_fp8_gemm(const Fp8TileArgs p) {
             if constexpr (j + 1 < FN) {
                 b[(j + 1) & 1] = load_b(codes_of(cur), j + 1);
                 static_for<CH>([&](auto qc) {
-                    if constexpr (decltype(qc)::value * (FN - 1) / CH == j) issue_codes(prv, kt + NSTAGE - 1, decltype(qc)::value);
+                    if constexpr (decltype(qc)::value * DJ / CH == j) issue_codes(prv, kt + NSTAGE - 1, decltype(qc)::value);
                 });
             } else {
                 // every operand of this step is in registers: the next step's have landed, by this wave's DMA and then by every wave's
@@ -327,7 +299,9 @@ template <bool GATED> pme_status launch_one(const Fp8GemmArgs& a, int id) {
         case 5: return launch_tile<64, 64, 2, 2, 2, 3, GATED>(a);
         case 6: return launch_tile<32, 64, 1, 2, 4, 3, GATED>(a);
         case 7: return launch_tile<32, 32, 1, 1, 4, 3, GATED>(a);
+        case 8: return launch_fp8_gemm_decode(a);
     }
+    if (id >= 10) return launch_fp8_gemm_kslice(a, id - 10);
     return PME_ERR_UNSUPPORTED_PATH;
 }
 

@@ -149,6 +149,8 @@ struct Fp8GemmArgs {
 };
 pme_status launch_fp8_gemm_generic(const Fp8GemmArgs& a);
 pme_status launch_fp8_gemm_mfma(const Fp8GemmArgs& a);
+pme_status launch_fp8_gemm_decode(const Fp8GemmArgs& a);
+pme_status launch_fp8_gemm_kslice(const Fp8GemmArgs& a, int tile);
 void set_fp8_tile_override(int id);
 
 // Lets `kern` be launched with up to `bytes` of dynamic LDS.  The attribute is set once per kernel and
