@@ -44,12 +44,17 @@ k_fp8_gemm_generic(const uint8_t* __restrict__ qx, const float* __restrict__ sx,
 }
 
 
+// 16 bytes a lane from a wave-uniform base and a byte offset per lane, as dma16; LDS place lds + AT.
+template <int AT> __device__ __forceinline__ void dma16_to(const void* sbase, uint32_t voff, uint32_t lds) {
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds), "n"(AT) : "memory", "scc");
+}
+
 constexpr int fp8_stage(int bm, int bn, int ks) { return ks * (bm + bn) * 128; }
 constexpr int fp8_scale_blocks(int bm, bool gated) { return (bm + 63) / 64 + (gated ? 2 : 1); }
 constexpr int fp8_lds(int bm, int bn, int ks, int nstage, bool gated) { return nstage * fp8_stage(bm, bn, ks) + 2 * 1024 * fp8_scale_blocks(bm, gated); }
 
 template <int BM, int BN, int WGM, int WGN, int KS, int NSTAGE, bool GATED>
-__global__ void __launch_bounds__(64 * WGM * WGN * KS)
+__global__ void __launch_bounds__(64 * WGM * WGN * KS, 2)
 k_fp8_gemm(const Fp8TileArgs p) {
     constexpr int NWW = WGM * WGN;                               // waves of a slice of K
     constexpr int WM = BM / WGM, WN = BN / WGN, FM = WM / 16, FN = WN / 16;
@@ -57,12 +62,18 @@ k_fp8_gemm(const Fp8TileArgs p) {
     constexpr int ROWS = BM + BN, STAGE = fp8_stage(BM, BN, KS), SLICE = ROWS * 128;
     constexpr int CH = ROWS / 8 / NWW;                           // DMA instructions per wave and stage
     constexpr int XB = (BM + 63) / 64, SBLKS = fp8_scale_blocks(BM, GATED), GROUP = SBLKS * 1024, SCALES = NSTAGE * STAGE;
-    constexpr int GS = 4 / KS;                                   // stages of a group of scales
-    constexpr int DJ = FN - 1 < 2 ? FN - 1 : 2;                  // regions of the K step that carry the DMA of a later one
-    static_assert(KS == 1 || KS == 2 || KS == 4, "a group of scales is whole stages");
-    static_assert(ROWS / 8 % NWW == 0 && BM % 8 == 0 && BO % 8 == 0, "whole DMA blocks for every wave, none across operands");
+    constexpr int GS = 4 / KS;                                   // steps of a group of scales
+    // Registers: accumulators, two steps' tokens, one step's weights.  Where they fit, a step's operands are loaded a step ahead.
+    constexpr bool AHEAD = 4 * FM * FN + 16 * FM + 8 * FN <= 176;
+    constexpr int DEPTH = AHEAD ? NSTAGE - 2 : NSTAGE - 1;       // stages in flight behind the one that a step's reads are from
+    constexpr int DJ = AHEAD ? FN : FN - 1 < 2 ? FN - 1 : 2;     // regions of a step that carry its DMA
+    constexpr int UNROLL = NSTAGE % 2 ? 2 * NSTAGE : NSTAGE;     // steps of a round, in which every place in LDS is a constant
+    static_assert(KS == 1 || KS == 2, "a group of scales is whole steps, two at least");
+    static_assert(ROWS / 8 % NWW == 0 && BM / 8 % NWW == 0 && BO / 8 % NWW == 0, "a DMA instruction of every wave is from one operand");
     static_assert(128 % WO == 0 && WM % 16 == 0 && WO % 16 == 0, "a wave's channels lie in one block of scales");
     static_assert(BO <= 128 || BO == 256, "a tile has the scales of one or two blocks of channels");
+    static_assert(DEPTH >= 1 && GS >= DEPTH, "a group of scales is older than the codes that the wait leaves in flight");
+    static_assert(FM * FN % 4 == 0 && FN % 2 == 0, "the sums in flight, and the fragments of weights, go round");
 
     extern __shared__ __align__(1024) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -81,23 +92,24 @@ k_fp8_gemm(const Fp8TileArgs p) {
         const int row = r < BM ? min(m0 + r, p.T - 1) : min(n0 + (b < BO ? b : b - BO), p.N - 1);
         voff[q] = (uint32_t)row * (uint32_t)p.K + (uint32_t)(((lane & 7) ^ swz16(r)) << 4);
     }
-    auto issue_codes = [&](int stage, int kt, int q) {           // K block beyond the last: the last again, which nobody reads
-        const int blk = w + NWW * q, kb = min(kt * KS + ks, groups - 1);
+    const uint32_t lds_w = __builtin_amdgcn_readfirstlane(lds0 + ks * SLICE + w * 1024);
+    auto issue_codes = [&](auto stage, auto qc, int kt) {        // K block beyond the last: the last again, which nobody reads
+        constexpr int q = decltype(qc)::value, blk = NWW * q;
         const uint8_t* base = blk < BM / 8 ? p.qx : (GATED && blk >= (BM + BO) / 8) ? p.qu : p.qw;
-        dma16(base + (int64_t)kb * 128, voff[q], __builtin_amdgcn_readfirstlane(lds0 + stage * STAGE + ks * SLICE + blk * 1024));
+        dma16_to<decltype(stage)::value * STAGE + blk * 1024>(base + (uint32_t)(min(kt * KS + ks, groups - 1) * 128), voff[q], lds_w);
     };
     // of scales: sixteen bytes, four K blocks, of a token or of a block of channels; group g goes to place g & 1
     const uint32_t rowb = (uint32_t)groups * 4;
     const u32x4 sx_buf = buffer_of(p.sx, (uint32_t)p.T * rowb), sw_buf = buffer_of(p.sw, (uint32_t)((p.N + 127) / 128) * rowb);
     const u32x4 su_buf = buffer_of(GATED ? p.su : p.sw, (uint32_t)((p.N + 127) / 128) * rowb);
+    static_assert(SBLKS <= NWW * KS, "a DMA instruction of scales a wave");
+    const uint32_t srow = (uint32_t)(wave < XB ? min(m0 + min(64 * wave + lane, BM - 1), p.T - 1) : min(n0 / 128 + min(lane, 1), (p.N - 1) / 128)) * rowb;
+    const uint32_t lds_s = __builtin_amdgcn_readfirstlane(lds0 + SCALES + wave * 1024);
     auto issue_scales = [&](int g) {
-#pragma unroll
-        for (int s = 0; s < SBLKS; ++s) {
-            if (s % (NWW * KS) != wave) continue;
-            const int row = s < XB ? min(m0 + min(64 * s + lane, BM - 1), p.T - 1) : min(n0 / 128 + min(lane, 1), (p.N - 1) / 128);
-            dma16_buffer(s < XB ? sx_buf : s == XB ? sw_buf : su_buf, (uint32_t)row * rowb + 16 * (uint32_t)g,
-                         __builtin_amdgcn_readfirstlane(lds0 + SCALES + (g & 1) * GROUP + s * 1024));
-        }
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds_s + (g & 1) * GROUP), at = srow + 16 * (uint32_t)g;
+        if (wave < XB) dma16_buffer(sx_buf, at, to);
+        else if (wave == XB) dma16_buffer(sw_buf, at, to);
+        else if (GATED && wave == XB + 1) dma16_buffer(su_buf, at, to);
     };
 
     f32x4 acc[FM][FN];
@@ -108,93 +120,166 @@ k_fp8_gemm(const Fp8TileArgs p) {
 
     const int r16 = lane & 15, kg = lane >> 4;
     // chunk 4 q + kg of a row is at position (kg ^ swz) ^ 4 q; rows 16 apart share their swizzle
-    const int aoff = (wm * WM + r16) * 128 + ((kg ^ swz16(r16)) << 4), boff = (BM + wn * WO + r16) * 128 + ((kg ^ swz16(r16)) << 4);
-    const int soff = 16 * (wm * WM + r16), swoff = XB * 1024 + 16 * ((n0 + wn * WO) / 128 - n0 / 128);      // the wave's block of channels within the tile
-    auto frag = [&](const unsigned char* lo, const unsigned char* hi) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(lo), b = *reinterpret_cast<const u32x4*>(hi);
+    const int c0 = ks * SLICE + r16 * 128 + ((kg ^ swz16(r16)) << 4);
+    const int a0 = c0 + wm * WM * 128, a1 = a0 ^ 64, b0 = c0 + (BM + wn * WO) * 128, b1 = b0 ^ 64;
+    const int soff = SCALES + 16 * (wm * WM + r16), swoff = SCALES + XB * 1024 + 16 * ((n0 + wn * WO) / 128 - n0 / 128);      // the wave's block of channels
+    auto frag = [&](int lo, int hi) {
+        const u32x4 a = *reinterpret_cast<const u32x4*>(smem + lo), b = *reinterpret_cast<const u32x4*>(smem + hi);
         return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
     };
-    // of the K step in stage st: byte offsets of the slice's codes, of its scales
-    auto codes_of = [&](int stage) { return stage * STAGE + ks * SLICE; };
-    auto scales_of = [&](int kt) { return SCALES + ((kt / GS) & 1) * GROUP + 4 * ((kt * KS + ks) & 3); };
-    auto load_a = [&](int at, int i) { return frag(smem + (at + aoff) + 2048 * i, smem + (at + (aoff ^ 64)) + 2048 * i); };
-    auto load_b = [&](int at, int j) {
-        const int row = 128 * (GATED && j >= FO ? BO + 16 * (j - FO) : 16 * j);
-        return frag(smem + (at + boff) + row, smem + (at + (boff ^ 64)) + row);
+    auto load_a = [&](auto stage, auto ic) {
+        constexpr int at = decltype(stage)::value * STAGE + 2048 * decltype(ic)::value;
+        return frag(a0 + at, a1 + at);
     };
-    i32x8 a[FM], b[2];
-    float sx[FM], sw, su, pw[FM], pu[FM];
-    auto load_sx = [&](int at, int i) { sx[i] = *reinterpret_cast<const float*>(smem + (at + soff) + 256 * i); };
-    auto load_sw = [&](int at) {
-        sw = *reinterpret_cast<const float*>(smem + (at + swoff));
-        if constexpr (GATED) su = *reinterpret_cast<const float*>(smem + (at + swoff) + 1024);
+    auto load_b = [&](auto stage, auto jc) {
+        constexpr int j = decltype(jc)::value, at = decltype(stage)::value * STAGE + 128 * (GATED && j >= FO ? BO + 16 * (j - FO) : 16 * j);
+        return frag(b0 + at, b1 + at);
     };
-
-    // prologue
-    issue_scales(0);
-    issue_scales(1);
+    // scales of a step: of the wave's tokens, of its block of channels; then their products
+    struct Scales { float x[FM], w, u; };
+    struct Products { float w[FM], u[FM]; };
+    auto scales_of = [&](int kt) { return ((kt / GS) & 1) * GROUP + 4 * ((kt * KS + ks) & 3); };
+    auto load_scales = [&](Scales& s, int kt) {
+        const int at = scales_of(kt);
+        s.w = *reinterpret_cast<const float*>(smem + (at + swoff));
+        if constexpr (GATED) s.u = *reinterpret_cast<const float*>(smem + (at + swoff) + 1024);
 #pragma unroll
-    for (int st = 0; st < NSTAGE; ++st)
-#pragma unroll
-        for (int q = 0; q < (st == NSTAGE - 1 ? 0 : CH); ++q) issue_codes(st, st, q);
-    wait_vm<(NSTAGE - 2) * CH>();
-    lds_barrier();
-    load_sw(scales_of(0));
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        a[i] = load_a(codes_of(0), i);
-        load_sx(scales_of(0), i);
-    }
-    b[0] = load_b(codes_of(0), 0);
-    static_assert(FN % 2 == 0, "the next step's first fragment goes to the same place");
-    int cur = 0;
-    for (int kt = 0; kt < KT; ++kt) {
-        const int nxt = cur == NSTAGE - 1 ? 0 : cur + 1, prv = cur == 0 ? NSTAGE - 1 : cur - 1;
-        if (kt > 0 && kt % GS == 0) issue_scales(kt / GS + 1);       // into the place that the last step has left
+        for (int i = 0; i < FM; ++i) s.x[i] = *reinterpret_cast<const float*>(smem + (at + soff) + 256 * i);
+    };
+    auto products = [&](const Scales& s, int kt) {
+        Products r;
         // a slice of K that has no block left in the last step works on its last block again, with a scale of zero
+        const bool live = KS == 1 || kt * KS + ks < groups;
+        const float sw = live ? s.w : 0.f, su = GATED && live ? s.u : 0.f;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const float v = KS == 1 || kt * KS + ks < groups ? sx[i] : 0.f;
-            pw[i] = v * sw;
-            pu[i] = GATED ? v * su : 0.f;
+            r.w[i] = s.x[i] * sw;
+            if constexpr (GATED) r.u[i] = s.x[i] * su;
         }
-        f32x4 t[4];
-        auto add = [&](auto mc) {
-            constexpr int m = decltype(mc)::value, i = m % FM, j = m / FM;
+        return r;
+    };
+    // Instruction m = j FM + i of a step, and the addition of its sum three instructions later, when it is there; the last three of a step
+    // are added in the next one.
+    f32x4 t[4] = {};
+    auto multiply = [&](auto mc, const i32x8& wv, const i32x8& xv) {
+        t[decltype(mc)::value & 3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+    };
+    auto add = [&](const Products& s, auto mc) {
+        constexpr int m = decltype(mc)::value, i = m % FM, j = m / FM;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[m & 3][e], GATED && j >= FO ? pu[i] : pw[i], acc[i][j][e]);
-        };
-        static_for<FN>([&](auto jc) {
-            constexpr int j = decltype(jc)::value;
-            if constexpr (j + 1 < FN) {
-                b[(j + 1) & 1] = load_b(codes_of(cur), j + 1);
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[m & 3][e], GATED && j >= FO ? s.u[i] : s.w[i], acc[i][j][e]);
+    };
+    auto add_behind = [&](const Products& before, const Products& now, auto mc) {
+        constexpr int m = decltype(mc)::value;
+        if constexpr (m < 3) add(before, std::integral_constant<int, FM * FN - 3 + m>{});
+        else add(now, std::integral_constant<int, m - 3>{});
+    };
+    Products before, now;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) before.w[i] = before.u[i] = 0.f;
+
+    issue_scales(0);
+    issue_scales(1);
+    static_for<DEPTH + (AHEAD ? 1 : 0)>([&](auto st) { static_for<CH>([&](auto qc) { issue_codes(st, qc, decltype(st)::value); }); });
+    constexpr std::integral_constant<int, 0> first{};
+    Scales s;
+    if constexpr (AHEAD) {
+        // Every operand of a step is in registers when the step begins, and is replaced by the next one's as it is used: a step's LDS
+        // reads have the whole of the step before to arrive in, and nothing waits for the last of them at the barrier.
+        i32x8 a[2][FM], b[FN];
+        wait_vm<DEPTH * CH>();
+        lds_barrier();
+        load_scales(s, 0);
+        static_for<FM>([&](auto ic) { a[0][decltype(ic)::value] = load_a(first, ic); });
+        static_for<FN>([&](auto jc) { b[decltype(jc)::value] = load_b(first, jc); });
+        auto step = [&](auto uc, int kt) {
+            constexpr int u = decltype(uc)::value;
+            constexpr std::integral_constant<int, (u + 1) % NSTAGE> nxt{};
+            constexpr std::integral_constant<int, (u + NSTAGE - 1) % NSTAGE> prv{};
+            // The next step's operands have landed, by this wave's DMA and then by every wave's.  This step's may still be on their way into
+            // other waves' registers; those of the step before were used there: their stage can be filled again, and the place of the
+            // scales before this group's.
+            wait_vm<(DEPTH - 1) * CH>();
+            asm volatile("s_barrier" ::: "memory");
+            if (kt > 0 && kt % GS == 0) issue_scales(kt / GS + 1);
+            now = products(s, kt);
+            load_scales(s, kt + 1);
+            static_for<FM>([&](auto ic) { a[(u + 1) & 1][decltype(ic)::value] = load_a(nxt, ic); });
+            static_for<FN>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
                 static_for<CH>([&](auto qc) {
-                    if constexpr (decltype(qc)::value * DJ / CH == j) issue_codes(prv, kt + NSTAGE - 1, decltype(qc)::value);
+                    if constexpr (decltype(qc)::value * DJ / CH == j) issue_codes(prv, qc, kt + NSTAGE - 1);
                 });
-            } else {
-                // every operand of this step is in registers: the next step's have landed, by this wave's DMA and then by every wave's
-                wait_vm<(NSTAGE - 2) * CH>();
-                lds_barrier();
-                b[0] = load_b(codes_of(nxt), 0);
-                load_sw(scales_of(kt + 1));
-            }
-            static_for<FM>([&](auto ic) {
-                constexpr int i = decltype(ic)::value, m = j * FM + i;
-                t[m & 3] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[j & 1], a[i], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-                if constexpr (j == FN - 1) {
-                    a[i] = load_a(codes_of(nxt), i);
-                    load_sx(scales_of(kt + 1), i);
-                }
-                if constexpr (m >= 3) add(std::integral_constant<int, m - 3>{});
-                __builtin_amdgcn_sched_barrier(0);
+                static_for<FM>([&](auto ic) {
+                    constexpr std::integral_constant<int, j * FM + decltype(ic)::value> m{};
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (m < 3) add_behind(before, now, m);
+                    multiply(m, b[j], a[u & 1][decltype(ic)::value]);
+                    if constexpr (decltype(ic)::value == FM - 1) b[j] = load_b(nxt, jc);
+                    if constexpr (m >= 3) add_behind(before, now, m);
+                });
             });
-        });
-        static_for<3>([&](auto rc) {
-            constexpr int m = FM * FN - 3 + decltype(rc)::value;
-            if constexpr (m >= 0) add(std::integral_constant<int, m>{});
-        });
-        cur = nxt;
+            before = now;
+        };
+        for (int kt = 0; kt < KT; kt += UNROLL)
+            static_for<UNROLL>([&](auto uc) {
+                if (decltype(uc)::value == 0 || kt + decltype(uc)::value < KT) step(uc, kt + decltype(uc)::value);
+            });
+    } else {
+        // Too many registers for that: the weights' fragments come one region ahead, the next step's first operands over the last region.
+        i32x8 a[FM], b[2];
+        wait_vm<(DEPTH - 1) * CH>();
+        lds_barrier();
+        load_scales(s, 0);
+        static_for<FM>([&](auto ic) { a[decltype(ic)::value] = load_a(first, ic); });
+        b[0] = load_b(first, first);
+        auto step = [&](auto uc, int kt) {
+            constexpr int u = decltype(uc)::value;
+            constexpr std::integral_constant<int, u % NSTAGE> cur{};
+            constexpr std::integral_constant<int, (u + 1) % NSTAGE> nxt{};
+            constexpr std::integral_constant<int, (u + NSTAGE - 1) % NSTAGE> prv{};
+            if (kt > 0 && kt % GS == 0) issue_scales(kt / GS + 1);       // into the place that the last step has left
+            now = products(s, kt);
+            static_for<FN>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                if constexpr (j + 1 < FN) {
+                    b[(j + 1) & 1] = load_b(cur, std::integral_constant<int, j + 1>{});
+                    static_for<CH>([&](auto qc) {
+                        if constexpr (decltype(qc)::value * DJ / CH == j) issue_codes(prv, qc, kt + NSTAGE - 1);
+                    });
+                } else {
+                    // every operand of this step is in registers: the next step's have landed, by this wave's DMA and then by every wave's
+                    wait_vm<(DEPTH - 1) * CH>();
+                    lds_barrier();
+                    b[0] = load_b(nxt, first);
+                    load_scales(s, kt + 1);
+                }
+                static_for<FM>([&](auto ic) {
+                    constexpr int i = decltype(ic)::value;
+                    constexpr std::integral_constant<int, j * FM + i> m{};
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (m < 3) add_behind(before, now, m);
+                    multiply(m, b[j & 1], a[i]);
+                    if constexpr (j == FN - 1) a[i] = load_a(nxt, ic);
+                    if constexpr (m >= 3) add_behind(before, now, m);
+                });
+            });
+            before = now;
+            // the additions stay in their step
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    f32x4& v = acc[i][j];
+                    asm volatile("" : "+v"(v));
+                }
+        };
+        for (int kt = 0; kt < KT; kt += UNROLL)
+            static_for<UNROLL>([&](auto uc) {
+                if (decltype(uc)::value == 0 || kt + decltype(uc)::value < KT) step(uc, kt + decltype(uc)::value);
+            });
     }
+    static_for<3>([&](auto mc) { add_behind(before, now, mc); });
     wait_vm<0>();
     lds_barrier();
 
@@ -294,12 +379,21 @@ template <bool GATED> pme_status launch_one(const Fp8GemmArgs& a, int id) {
     switch (id) {
         case 1: return launch_tile<256, 256, 4, 2, 1, 2, GATED>(a);
         case 2: return launch_tile<128, 256, 2, 4, 1, 3, GATED>(a);
-        case 3: return launch_tile<128, 128, 2, 2, 2, 2, GATED>(a);
-        case 4: return launch_tile<64, 128, 2, 2, 2, 2, GATED>(a);
-        case 5: return launch_tile<64, 64, 2, 2, 2, 3, GATED>(a);
-        case 6: return launch_tile<32, 64, 1, 2, 4, 3, GATED>(a);
-        case 7: return launch_tile<32, 32, 1, 1, 4, 3, GATED>(a);
+        case 3: return launch_tile<128, 128, 4, 2, 1, 4, GATED>(a);
+        case 4: return launch_tile<64, 128, 2, 2, 1, 4, GATED>(a);
+        case 5: return launch_tile<64, 64, 2, 2, 2, 4, GATED>(a);
+        case 6: return launch_tile<64, 64, 2, 2, 1, 4, GATED>(a);
+        case 7: return launch_tile<64, 128, 2, 2, 2, 3, GATED>(a);
         case 8: return launch_fp8_gemm_decode(a);
+    }
+    switch (id) {
+        case 40: return launch_tile<128, 64, 4, 1, 1, 4, GATED>(a);
+        case 41: return launch_tile<128, 128, 2, 4, 1, 4, GATED>(a);
+        case 42: return launch_tile<128, 128, 2, 2, 1, 4, GATED>(a);
+        case 43: return launch_tile<64, 64, 2, 2, 1, 6, GATED>(a);
+        case 44: return launch_tile<64, 128, 2, 4, 1, 4, GATED>(a);
+        case 45: return launch_tile<64, 64, 2, 2, 2, 3, GATED>(a);
+        case 46: return launch_tile<64, 64, 1, 2, 2, 4, GATED>(a);
     }
     if (id >= 10) return launch_fp8_gemm_kslice(a, id - 10);
     return PME_ERR_UNSUPPORTED_PATH;

@@ -27,9 +27,8 @@ k_fp8_gemm_kslice(const Fp8TileArgs p) {
     constexpr int FM = (AR + 15) / 16, FN = BN / 16, BO = GATED ? BN / 2 : BN, FO = BO / 16, ROWS = AR + BN;
     constexpr int CH = ROWS / 8;                                 // DMA instructions of a K block
     constexpr int STAGE = ROWS * 128, SCALES = NSTAGE * STAGE, GROUP = fp8_kslice_group(AR, GATED), RING = fp8_kslice_ring(AR, BN, NSTAGE, GATED);
-    constexpr int SROWS = AR + (GATED ? 2 : 1);                  // rows of scales: tokens, blocks of channels
     static_assert((AR == 8 || AR % 16 == 0) && BN % (GATED ? 32 : 16) == 0 && 128 % BO == 0, "whole fragments; a tile's channels have one scale a matrix");
-    static_assert(SROWS <= 64 && (NSTAGE - 1) * CH + 2 <= 63, "one DMA a group of scales; wait counts fit vmcnt");
+    static_assert(AR <= 64 && (NSTAGE - 1) * CH + 2 <= 63, "one DMA for the tokens' scales; wait counts fit vmcnt");
     static_assert(NSTAGE <= 6, "a group of scales, issued four steps before its first reader, is older than the codes that the wait leaves in flight");
     extern __shared__ __align__(1024) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -50,7 +49,7 @@ k_fp8_gemm_kslice(const Fp8TileArgs p) {
     }
     // step s of this wave (beyond its last one the last of all K blocks, which nobody reads)
     auto issue_codes = [&](int stage, int s) {
-        const int64_t at = (int64_t)min(first + s, groups - 1) * 128;
+        const int64_t at = (int64_t)__builtin_amdgcn_readfirstlane(min(first + s, groups - 1)) * 128;
 #pragma unroll
         for (int q = 0; q < CH; ++q)
             dma16((8 * q < AR ? p.qx : GATED && 8 * q >= AR + BO ? p.qu : p.qw) + at, voff[q], __builtin_amdgcn_readfirstlane(lds0 + stage * STAGE + q * 1024));
@@ -63,8 +62,10 @@ k_fp8_gemm_kslice(const Fp8TileArgs p) {
     auto issue_scales = [&](int g) {
         const uint32_t at = (uint32_t)min(first + 4 * g, groups - 1) * 4, to = __builtin_amdgcn_readfirstlane(lds0 + SCALES + (g & 1) * GROUP);
         if (lane < AR) dma16_buffer(sx_buf, srow + at, to);
-        if (lane == AR) dma16_buffer(sw_buf, wrow + at, to);
-        if (GATED && lane == AR + 1) dma16_buffer(su_buf, wrow + at, to);
+        if (lane == 0) {
+            dma16_buffer(sw_buf, wrow + at, to + 16 * AR);
+            if constexpr (GATED) dma16_buffer(su_buf, wrow + at, to + 16 * AR + 16);
+        }
     };
 
     f32x4 acc[FM][FN];
@@ -179,6 +180,20 @@ template <bool GATED> pme_status launch_of(const Fp8GemmArgs& a, int id) {
         case 6: return launch_kslice<8, 32, 4, 3, GATED>(a);
         case 7: return launch_kslice<16, 64, 4, 3, GATED>(a);
         case 8: return launch_kslice<32, 64, 4, 3, GATED>(a);
+        case 9: return launch_kslice<16, 32, 4, 3, GATED>(a);
+        case 10: return launch_kslice<32, 32, 4, 2, GATED>(a);
+        case 11: return launch_kslice<32, 64, 4, 2, GATED>(a);
+        case 12: return launch_kslice<8, 64, 4, 2, GATED>(a);
+        case 13: return launch_kslice<8, 32, 2, 6, GATED>(a);
+        case 14: return launch_kslice<16, 32, 4, 2, GATED>(a);
+        case 15: return launch_kslice<8, 32, 4, 2, GATED>(a);
+        case 16: return launch_kslice<16, 64, 2, 3, GATED>(a);
+        case 17: return launch_kslice<32, 64, 2, 3, GATED>(a);
+        case 18: return launch_kslice<32, 32, 2, 3, GATED>(a);
+        case 19: return launch_kslice<48, 32, 4, 2, GATED>(a);
+        case 20: return launch_kslice<64, 32, 4, 2, GATED>(a);
+        case 21: return launch_kslice<64, 64, 2, 2, GATED>(a);
+        case 22: return launch_kslice<64, 64, 4, 2, GATED>(a);
     }
     return PME_ERR_UNSUPPORTED_PATH;
 }

@@ -278,7 +278,7 @@ def test_fp8_gated_gemm(T, K, N):
 
 
 # every tile, forced: one K block, K blocks that fill neither a stage nor a group of four scales, several tiles with ragged ends
-TILES = range(201, 208)
+TILES = [*range(201, 208), *range(240, 247)]
 TILE_SHAPES = [(1, 128, 16), (40, 384, 72), (300, 640, 530), (257, 1152, 385), (96, 2432, 128)]
 
 
@@ -308,7 +308,7 @@ def test_fp8_decode(T, K, N):
 
 
 # waves that split K: fewer blocks than waves, uneven shares, several groups of scales a wave, the ring filled several times
-KSLICE = range(210, 219)
+KSLICE = range(210, 233)
 
 
 @pytest.mark.parametrize("T,K,N", [(1, 128, 1), (8, 384, 33), (7, 8320, 40), (40, 1152, 140), (33, 12416, 72), (16, 6144, 130)])
