@@ -44,9 +44,10 @@ k_fp8_gemm_generic(const uint8_t* __restrict__ qx, const float* __restrict__ sx,
 }
 
 
-// 16 bytes a lane from a wave-uniform base and a byte offset per lane, as dma16; LDS place lds + AT.
-template <int AT> __device__ __forceinline__ void dma16_to(const void* sbase, uint32_t voff, uint32_t lds) {
-    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds), "n"(AT) : "memory", "scc");
+// 16 bytes a lane from a buffer, at a byte offset per lane plus a wave-uniform one, to LDS place lds + AT; bytes beyond the buffer's end
+// arrive as zeros.
+template <int AT> __device__ __forceinline__ void dma16_to(u32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
+    asm volatile("s_add_u32 m0, %3, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(voff), "s"(rsrc), "s"(soff), "s"(lds), "n"(AT) : "memory", "scc");
 }
 
 constexpr int fp8_stage(int bm, int bn, int ks) { return ks * (bm + bn) * 128; }
@@ -85,18 +86,29 @@ k_fp8_gemm(const Fp8TileArgs p) {
 
     // DMA of codes: block blk is rows 8 blk .. 8 blk + 7 of the wave's slice (tokens, channels, gated: the second matrix's channels);
     // lane L fills chunk position L % 8 of row L / 8, which holds chunk (L % 8) ^ swz
-    uint32_t voff[CH];
+    // (not AHEAD: after the tokens, of every column of waves the weights of its first regions, then those of its last ones)
+    constexpr int CHX = BM / 8 / NWW;
+    auto block_of = [](int q) {                                  // first block of the NWW that the q-th instructions fill
+        if (AHEAD || q < CHX) return NWW * q;
+        const int c = (q - CHX) % WGN, h = (q - CHX) / WGN;
+        return (BM + (GATED ? h * BO + c * (WN / 2) : c * WN + h * (WN / 2))) / 8;
+    };
+    static_assert(AHEAD || (WN / 2 / 8 == NWW && NSTAGE == 2 && KS == 1), "half the weights of a column of waves an instruction");
+    static_assert(NWW % 2 == 0, "every block of a wave has the same swizzle");
+    const uint32_t lane_off = (uint32_t)(lane >> 3) * (uint32_t)p.K + (uint32_t)(((lane & 7) ^ swz16(8 * w + (lane >> 3))) << 4);
+    const u32x4 x_buf = buffer_of(p.qx, (uint32_t)p.T * (uint32_t)p.K), w_buf = buffer_of(p.qw, (uint32_t)p.N * (uint32_t)p.K);
+    const u32x4 u_buf = buffer_of(GATED ? p.qu : p.qw, (uint32_t)p.N * (uint32_t)p.K);
+    uint32_t row_off[CH];                                        // of the block's first row (rows beyond the last: zeros, or any)
 #pragma unroll
     for (int q = 0; q < CH; ++q) {
-        const int r = 8 * (w + NWW * q) + (lane >> 3), b = r - BM;
-        const int row = r < BM ? min(m0 + r, p.T - 1) : min(n0 + (b < BO ? b : b - BO), p.N - 1);
-        voff[q] = (uint32_t)row * (uint32_t)p.K + (uint32_t)(((lane & 7) ^ swz16(r)) << 4);
+        const int r = 8 * (w + block_of(q)), b = r - BM;
+        row_off[q] = __builtin_amdgcn_readfirstlane((uint32_t)(r < BM ? m0 + r : n0 + (b < BO ? b : b - BO)) * (uint32_t)p.K);
     }
     const uint32_t lds_w = __builtin_amdgcn_readfirstlane(lds0 + ks * SLICE + w * 1024);
     auto issue_codes = [&](auto stage, auto qc, int kt) {        // K block beyond the last: the last again, which nobody reads
-        constexpr int q = decltype(qc)::value, blk = NWW * q;
-        const uint8_t* base = blk < BM / 8 ? p.qx : (GATED && blk >= (BM + BO) / 8) ? p.qu : p.qw;
-        dma16_to<decltype(stage)::value * STAGE + blk * 1024>(base + (uint32_t)(min(kt * KS + ks, groups - 1) * 128), voff[q], lds_w);
+        constexpr int q = decltype(qc)::value, blk = block_of(q);
+        const uint32_t at = lane_off + (uint32_t)(min(kt * KS + ks, groups - 1) * 128);
+        dma16_to<decltype(stage)::value * STAGE + blk * 1024>(blk < BM / 8 ? x_buf : (GATED && blk >= (BM + BO) / 8) ? u_buf : w_buf, at, row_off[q], lds_w);
     };
     // of scales: sixteen bytes, four K blocks, of a token or of a block of channels; group g goes to place g & 1
     const uint32_t rowb = (uint32_t)groups * 4;
@@ -180,13 +192,13 @@ k_fp8_gemm(const Fp8TileArgs p) {
 
     issue_scales(0);
     issue_scales(1);
-    static_for<DEPTH + (AHEAD ? 1 : 0)>([&](auto st) { static_for<CH>([&](auto qc) { issue_codes(st, qc, decltype(st)::value); }); });
     constexpr std::integral_constant<int, 0> first{};
     Scales s;
     if constexpr (AHEAD) {
         // Every operand of a step is in registers when the step begins, and is replaced by the next one's as it is used: a step's LDS
         // reads have the whole of the step before to arrive in, and nothing waits for the last of them at the barrier.
         i32x8 a[2][FM], b[FN];
+        static_for<DEPTH + 1>([&](auto st) { static_for<CH>([&](auto qc) { issue_codes(st, qc, decltype(st)::value); }); });
         wait_vm<DEPTH * CH>();
         lds_barrier();
         load_scales(s, 0);
@@ -227,32 +239,51 @@ k_fp8_gemm(const Fp8TileArgs p) {
             });
     } else {
         // Too many registers for that: the weights' fragments come one region ahead, the next step's first operands over the last region.
+        // Two stages, each in two parts: the tokens and the weights of the first half of the regions, and the weights of the other half.
+        // Every part is filled again as soon as it has been read, half a step or a whole one before the step that last read it ends, and
+        // has more than a step to land.
+        constexpr int G1 = CHX + WGN, H = FN / 2;                // DMA instructions of the first part; its regions
         i32x8 a[FM], b[2];
-        wait_vm<(DEPTH - 1) * CH>();
+        auto issue_part = [&](auto part, auto stage, int kt, auto from, auto to) {       // instructions [from, to) of the part
+            static_for<decltype(to)::value - decltype(from)::value>([&](auto qc) {
+                issue_codes(stage, std::integral_constant<int, decltype(part)::value * G1 + decltype(from)::value + decltype(qc)::value>{}, kt);
+            });
+        };
+        constexpr std::integral_constant<int, 1> second{};
+        constexpr std::integral_constant<int, G1> g1{};
+        constexpr std::integral_constant<int, CH - G1> g2{};
+        issue_part(first, first, 0, first, g1);
+        issue_part(second, first, 0, first, g2);
+        issue_part(first, second, 1, first, g1);
+        wait_vm<CH>();
         lds_barrier();
         load_scales(s, 0);
         static_for<FM>([&](auto ic) { a[decltype(ic)::value] = load_a(first, ic); });
         b[0] = load_b(first, first);
         auto step = [&](auto uc, int kt) {
-            constexpr int u = decltype(uc)::value;
-            constexpr std::integral_constant<int, u % NSTAGE> cur{};
-            constexpr std::integral_constant<int, (u + 1) % NSTAGE> nxt{};
-            constexpr std::integral_constant<int, (u + NSTAGE - 1) % NSTAGE> prv{};
+            constexpr std::integral_constant<int, decltype(uc)::value & 1> cur{};
+            constexpr std::integral_constant<int, 1 - cur> nxt{};
             if (kt > 0 && kt % GS == 0) issue_scales(kt / GS + 1);       // into the place that the last step has left
             now = products(s, kt);
             static_for<FN>([&](auto jc) {
                 constexpr int j = decltype(jc)::value;
-                if constexpr (j + 1 < FN) {
-                    b[(j + 1) & 1] = load_b(cur, std::integral_constant<int, j + 1>{});
-                    static_for<CH>([&](auto qc) {
-                        if constexpr (decltype(qc)::value * DJ / CH == j) issue_codes(prv, qc, kt + NSTAGE - 1);
-                    });
-                } else {
-                    // every operand of this step is in registers: the next step's have landed, by this wave's DMA and then by every wave's
-                    wait_vm<(DEPTH - 1) * CH>();
+                // One part behind the newest CH instructions has landed, by this wave's DMA and then by every wave's: before region H - 1
+                // the second part of this step, before the last region the first part of the next one.  What lies before the fragment
+                // that this region multiplies has been read by every wave.
+                if constexpr (j == H - 1 || j == FN - 1) {
+                    wait_vm<CH>();
                     lds_barrier();
+                }
+                if constexpr (j + 1 < FN) b[(j + 1) & 1] = load_b(cur, std::integral_constant<int, j + 1>{});
+                else {
                     b[0] = load_b(nxt, first);
                     load_scales(s, kt + 1);
+                }
+                if constexpr (j == 0) issue_part(second, nxt, kt + 1, first, g2);
+                if constexpr (j >= H - 1 && j < H + 2) {
+                    constexpr std::integral_constant<int, (j - H + 1) * G1 / 3> from{};
+                    constexpr std::integral_constant<int, (j - H + 2) * G1 / 3> to{};
+                    issue_part(first, cur, kt + 2, from, to);
                 }
                 static_for<FM>([&](auto ic) {
                     constexpr int i = decltype(ic)::value;
