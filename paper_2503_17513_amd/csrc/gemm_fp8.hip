@@ -54,7 +54,7 @@ constexpr int fp8_stage(int bm, int bn, int ks) { return ks * (bm + bn) * 128; }
 constexpr int fp8_scale_blocks(int bm, bool gated) { return (bm + 63) / 64 + (gated ? 2 : 1); }
 constexpr int fp8_lds(int bm, int bn, int ks, int nstage, bool gated) { return nstage * fp8_stage(bm, bn, ks) + 2 * 1024 * fp8_scale_blocks(bm, gated); }
 
-template <int BM, int BN, int WGM, int WGN, int KS, int NSTAGE, bool GATED>
+template <int BM, int BN, int WGM, int WGN, int KS, int NSTAGE, bool AHEAD, bool GATED>
 __global__ void __launch_bounds__(64 * WGM * WGN * KS, 2)
 k_fp8_gemm(const Fp8TileArgs p) {
     constexpr int NWW = WGM * WGN;                               // waves of a slice of K
@@ -64,8 +64,6 @@ k_fp8_gemm(const Fp8TileArgs p) {
     constexpr int CH = ROWS / 8 / NWW;                           // DMA instructions per wave and stage
     constexpr int XB = (BM + 63) / 64, SBLKS = fp8_scale_blocks(BM, GATED), GROUP = SBLKS * 1024, SCALES = NSTAGE * STAGE;
     constexpr int GS = 4 / KS;                                   // steps of a group of scales
-    // Registers: accumulators, two steps' tokens, one step's weights.  Where they fit, a step's operands are loaded a step ahead.
-    constexpr bool AHEAD = 4 * FM * FN + 16 * FM + 8 * FN <= 176;
     constexpr int DEPTH = AHEAD ? NSTAGE - 2 : NSTAGE - 1;       // stages in flight behind the one that a step's reads are from
     constexpr int DJ = AHEAD ? FN : FN - 1 < 2 ? FN - 1 : 2;     // regions of a step that carry its DMA
     constexpr int UNROLL = NSTAGE % 2 ? 2 * NSTAGE : NSTAGE;     // steps of a round, in which every place in LDS is a constant
@@ -377,13 +375,13 @@ k_fp8_gemm(const Fp8TileArgs p) {
     }
 }
 
-template <int BM, int BN, int WGM, int WGN, int KS, int NSTAGE, bool GATED> pme_status launch_tile(const Fp8GemmArgs& a) {
+template <int BM, int BN, int WGM, int WGN, int KS, int NSTAGE, bool AHEAD, bool GATED> pme_status launch_tile(const Fp8GemmArgs& a) {
     if (a.dry) {
         if (a.plan) {
             // the instantiation's name as a profiler prints it
             static const std::string name = [] {
                 char buf[96];
-                snprintf(buf, sizeof buf, "k_fp8_gemm<%d, %d, %d, %d, %d, %d, %s>", BM, BN, WGM, WGN, KS, NSTAGE, GATED ? "true" : "false");
+                snprintf(buf, sizeof buf, "k_fp8_gemm<%d, %d, %d, %d, %d, %d, %s, %s>", BM, BN, WGM, WGN, KS, NSTAGE, AHEAD ? "true" : "false", GATED ? "true" : "false");
                 return std::string(buf);
             }();
             *a.plan = name.c_str();
@@ -394,7 +392,7 @@ template <int BM, int BN, int WGM, int WGN, int KS, int NSTAGE, bool GATED> pme_
     constexpr int lds = fp8_lds(BM, BN, KS, NSTAGE, GATED);
     static_assert(lds <= 160 * 1024, "LDS of a compute unit");
     const int tiles_m = (int)((a.T + BM - 1) / BM), tiles_n = (int)((a.N + BO - 1) / BO);
-    auto kern = k_fp8_gemm<BM, BN, WGM, WGN, KS, NSTAGE, GATED>;
+    auto kern = k_fp8_gemm<BM, BN, WGM, WGN, KS, NSTAGE, AHEAD, GATED>;
     static std::atomic<uint32_t> done;
     if (allow_dynamic_lds(kern, lds, done) != PME_OK) return PME_ERR_HIP;
     const int vec = (a.N % 8 == 0 && a.ldy % 8 == 0 && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0) ? 1 : 0;
@@ -408,23 +406,20 @@ int g_fp8_tile_override = 0;
 
 template <bool GATED> pme_status launch_one(const Fp8GemmArgs& a, int id) {
     switch (id) {
-        case 1: return launch_tile<256, 256, 4, 2, 1, 2, GATED>(a);
-        case 2: return launch_tile<128, 256, 2, 4, 1, 3, GATED>(a);
-        case 3: return launch_tile<128, 128, 4, 2, 1, 4, GATED>(a);
-        case 4: return launch_tile<64, 128, 2, 2, 1, 4, GATED>(a);
-        case 5: return launch_tile<64, 64, 2, 2, 2, 4, GATED>(a);
-        case 6: return launch_tile<64, 64, 2, 2, 1, 4, GATED>(a);
-        case 7: return launch_tile<64, 128, 2, 2, 2, 3, GATED>(a);
+        case 1: return launch_tile<256, 256, 4, 2, 1, 2, false, GATED>(a);
+        case 2: return launch_tile<128, 256, 2, 4, 1, 3, true, GATED>(a);
+        case 3: return launch_tile<128, 128, 4, 2, 1, 4, true, GATED>(a);
+        case 4: return launch_tile<128, 128, 2, 4, 1, 4, true, GATED>(a);
+        case 5: return launch_tile<64, 64, 2, 2, 2, 4, true, GATED>(a);
+        case 6: return launch_tile<64, 64, 2, 2, 1, 4, true, GATED>(a);
+        case 7: return launch_tile<64, 128, 2, 4, 1, 4, true, GATED>(a);
         case 8: return launch_fp8_gemm_decode(a);
-    }
-    switch (id) {
-        case 40: return launch_tile<128, 64, 4, 1, 1, 4, GATED>(a);
-        case 41: return launch_tile<128, 128, 2, 4, 1, 4, GATED>(a);
-        case 42: return launch_tile<128, 128, 2, 2, 1, 4, GATED>(a);
-        case 43: return launch_tile<64, 64, 2, 2, 1, 6, GATED>(a);
-        case 44: return launch_tile<64, 128, 2, 4, 1, 4, GATED>(a);
-        case 45: return launch_tile<64, 64, 2, 2, 2, 3, GATED>(a);
-        case 46: return launch_tile<64, 64, 1, 2, 2, 4, GATED>(a);
+        case 40: return launch_tile<128, 128, 2, 2, 1, 2, false, GATED>(a);
+        case 41: return launch_tile<128, 256, 4, 2, 1, 2, false, GATED>(a);
+        case 42: return launch_tile<256, 128, 4, 2, 1, 3, true, GATED>(a);
+        case 43: return launch_tile<64, 128, 2, 2, 1, 3, true, GATED>(a);
+        case 45: return launch_tile<64, 256, 1, 4, 1, 2, false, GATED>(a);
+        case 46: return launch_tile<64, 64, 2, 2, 1, 3, true, GATED>(a);
     }
     if (id >= 10) return launch_fp8_gemm_kslice(a, id - 10);
     return PME_ERR_UNSUPPORTED_PATH;
