@@ -241,6 +241,8 @@ k_fp8_gemm(const Fp8TileArgs p) {
         // Every part is filled again as soon as it has been read, half a step or a whole one before the step that last read it ends, and
         // has more than a step to land.
         constexpr int G1 = CHX + WGN, H = FN / 2;                // DMA instructions of the first part; its regions
+        constexpr int R = H < 3 ? H : 3;                         // regions that carry its refill, all before the last one's wait
+        static_assert(H >= 2, "the second part's refill is issued before the wait that counts it");
         i32x8 a[FM], b[2];
         auto issue_part = [&](auto part, auto stage, int kt, auto from, auto to) {       // instructions [from, to) of the part
             static_for<decltype(to)::value - decltype(from)::value>([&](auto qc) {
@@ -278,9 +280,9 @@ k_fp8_gemm(const Fp8TileArgs p) {
                     load_scales(s, kt + 1);
                 }
                 if constexpr (j == 0) issue_part(second, nxt, kt + 1, first, g2);
-                if constexpr (j >= H - 1 && j < H + 2) {
-                    constexpr std::integral_constant<int, (j - H + 1) * G1 / 3> from{};
-                    constexpr std::integral_constant<int, (j - H + 2) * G1 / 3> to{};
+                if constexpr (j >= H - 1 && j < H - 1 + R) {
+                    constexpr std::integral_constant<int, (j - H + 1) * G1 / R> from{};
+                    constexpr std::integral_constant<int, (j - H + 2) * G1 / R> to{};
                     issue_part(first, cur, kt + 2, from, to);
                 }
                 static_for<FM>([&](auto ic) {
@@ -416,10 +418,10 @@ template <bool GATED> pme_status launch_one(const Fp8GemmArgs& a, int id) {
         case 8: return launch_fp8_gemm_decode(a);
         case 40: return launch_tile<128, 128, 2, 2, 1, 2, false, GATED>(a);
         case 41: return launch_tile<128, 256, 4, 2, 1, 2, false, GATED>(a);
-        case 42: return launch_tile<256, 128, 4, 2, 1, 3, true, GATED>(a);
-        case 43: return launch_tile<64, 128, 2, 2, 1, 3, true, GATED>(a);
-        case 45: return launch_tile<64, 256, 1, 4, 1, 2, false, GATED>(a);
-        case 46: return launch_tile<64, 64, 2, 2, 1, 3, true, GATED>(a);
+        case 42: return launch_tile<64, 128, 2, 2, 1, 2, false, GATED>(a);
+        case 43: return launch_tile<128, 64, 4, 1, 1, 2, false, GATED>(a);
+        case 45: return launch_tile<256, 128, 8, 1, 1, 2, false, GATED>(a);
+        case 46: return launch_tile<64, 64, 2, 2, 1, 6, true, GATED>(a);
     }
     if (id >= 10) return launch_fp8_gemm_kslice(a, id - 10);
     return PME_ERR_UNSUPPORTED_PATH;
