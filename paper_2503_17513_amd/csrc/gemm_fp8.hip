@@ -44,12 +44,6 @@ k_fp8_gemm_generic(const uint8_t* __restrict__ qx, const float* __restrict__ sx,
 }
 
 
-// 16 bytes a lane from a buffer, at a byte offset per lane plus a wave-uniform one, to LDS place lds + AT; bytes beyond the buffer's end
-// arrive as zeros.
-template <int AT> __device__ __forceinline__ void dma16_to(u32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
-    asm volatile("s_add_u32 m0, %3, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(voff), "s"(rsrc), "s"(soff), "s"(lds), "n"(AT) : "memory", "scc");
-}
-
 constexpr int fp8_stage(int bm, int bn, int ks) { return ks * (bm + bn) * 128; }
 constexpr int fp8_scale_blocks(int bm, bool gated) { return (bm + 63) / 64 + (gated ? 2 : 1); }
 constexpr int fp8_lds(int bm, int bn, int ks, int nstage, bool gated) { return nstage * fp8_stage(bm, bn, ks) + 2 * 1024 * fp8_scale_blocks(bm, gated); }

@@ -38,21 +38,20 @@ k_fp8_gemm_kslice(const Fp8TileArgs p) {
     const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)wave * groups / NW));
     const int steps = __builtin_amdgcn_readfirstlane((int)((int64_t)(wave + 1) * groups / NW) - first);
     const int ring = wave * RING;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(PME_AS3 unsigned char*)smem + ring;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(PME_AS3 unsigned char*)smem + ring);
 
-    uint32_t voff[CH];
-#pragma unroll
-    for (int q = 0; q < CH; ++q) {
-        const int r = 8 * q + (lane >> 3), b = r - AR;
-        const int row = r < AR ? min(m0 + r, p.T - 1) : min(n0 + (b < BO ? b : b - BO), p.N - 1);
-        voff[q] = (uint32_t)row * (uint32_t)p.K + (uint32_t)(((lane & 7) ^ swz16(r)) << 4);
-    }
-    // step s of this wave (beyond its last one the last of all K blocks, which nobody reads)
-    auto issue_codes = [&](int stage, int s) {
-        const int64_t at = (int64_t)__builtin_amdgcn_readfirstlane(min(first + s, groups - 1)) * 128;
-#pragma unroll
-        for (int q = 0; q < CH; ++q)
-            dma16((8 * q < AR ? p.qx : GATED && 8 * q >= AR + BO ? p.qu : p.qw) + at, voff[q], __builtin_amdgcn_readfirstlane(lds0 + stage * STAGE + q * 1024));
+    const uint32_t lane_off = (uint32_t)(lane >> 3) * (uint32_t)p.K + (uint32_t)(((lane & 7) ^ swz16(lane >> 3)) << 4);
+    const u32x4 x_buf = buffer_of(p.qx, (uint32_t)p.T * (uint32_t)p.K), w_buf = buffer_of(p.qw, (uint32_t)p.N * (uint32_t)p.K);
+    const u32x4 u_buf = buffer_of(GATED ? p.qu : p.qw, (uint32_t)p.N * (uint32_t)p.K);
+    // step s of this wave (beyond its last one the last of all K blocks, which nobody reads); rows beyond the last are zeros, or any
+    auto issue_codes = [&](auto stage, int s) {
+        const uint32_t at = lane_off + (uint32_t)(min(first + s, groups - 1) * 128);
+        static_for<CH>([&](auto qc) {
+            constexpr int q = decltype(qc)::value, r = 8 * q, b = r - AR;
+            const uint32_t row = (uint32_t)(r < AR ? m0 + r : n0 + (b < BO ? b : b - BO)) * (uint32_t)p.K;
+            // the odd blocks' rows have the other half of the swizzles
+            dma16_to<decltype(stage)::value * STAGE + q * 1024>(r < AR ? x_buf : GATED && b >= BO ? u_buf : w_buf, (q & 1) ? at ^ 64 : at, row, lds0);
+        });
     };
     // scales of steps 4 g .. 4 g + 3: sixteen bytes of every token and block of channels, those beyond the end of the array as zeros
     const uint32_t rowb = (uint32_t)groups * 4, wrow = (uint32_t)(n0 / 128) * rowb;
@@ -75,35 +74,35 @@ k_fp8_gemm_kslice(const Fp8TileArgs p) {
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     const int r16 = lane & 15, kg = lane >> 4, ra = AR == 8 ? r16 & 7 : r16;
     // a tile of 8 tokens repeats them over the fragment's rows: the surplus results are never stored
-    const int aoff = ring + ra * 128 + ((kg ^ swz16(ra)) << 4), boff = ring + (AR + r16) * 128 + ((kg ^ swz16(AR + r16)) << 4);
-    auto frag = [&](int at) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(smem + at), b = *reinterpret_cast<const u32x4*>(smem + (at ^ 64));
+    const int a0 = ring + ra * 128 + ((kg ^ swz16(ra)) << 4), a1 = a0 ^ 64, b0 = ring + (AR + r16) * 128 + ((kg ^ swz16(AR + r16)) << 4), b1 = b0 ^ 64;
+    auto frag = [&](int lo, int hi) {
+        const u32x4 a = *reinterpret_cast<const u32x4*>(smem + lo), b = *reinterpret_cast<const u32x4*>(smem + hi);
         return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
     };
 
     if (steps > 0) {
         issue_scales(0);
         issue_scales(1);
-#pragma unroll
-        for (int st = 0; st < NSTAGE - 1; ++st) issue_codes(st, st);
-        int cur = 0;
-        for (int s = 0; s < steps; ++s) {
+        static_for<NSTAGE - 1>([&](auto st) { issue_codes(st, decltype(st)::value); });
+        auto step = [&](auto uc, int s) {
+            constexpr int at = decltype(uc)::value * STAGE;
+            constexpr std::integral_constant<int, (decltype(uc)::value + NSTAGE - 1) % NSTAGE> prv{};
             // the fragments of the step before are in registers (their reads have been waited for): its stage, and every fourth step
             // its group of scales, can be filled again
             if (s > 0 && (s & 3) == 0) issue_scales((s >> 2) + 1);
-            issue_codes(cur == 0 ? NSTAGE - 1 : cur - 1, s + NSTAGE - 1);
+            issue_codes(prv, s + NSTAGE - 1);
             wait_vm<(NSTAGE - 1) * CH>();
-            const int sc = ring + SCALES + ((s >> 2) & 1) * GROUP + 4 * (s & 3), at = cur * STAGE;
+            const int sc = ring + SCALES + ((s >> 2) & 1) * GROUP + 4 * (s & 3);
             const float sw = *reinterpret_cast<const float*>(smem + sc + 16 * AR), su = GATED ? *reinterpret_cast<const float*>(smem + sc + 16 * (AR + 1)) : 0.f;
             float sx[FM];
             i32x8 a[FM], b[FN];
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                a[i] = frag(at + aoff + 2048 * i);
+                a[i] = frag(a0 + at + 2048 * i, a1 + at + 2048 * i);
                 sx[i] = *reinterpret_cast<const float*>(smem + sc + 16 * (ra + 16 * i));
             }
 #pragma unroll
-            for (int j = 0; j < FN; ++j) b[j] = frag(at + boff + 2048 * j);
+            for (int j = 0; j < FN; ++j) b[j] = frag(b0 + at + 2048 * j, b1 + at + 2048 * j);
 #pragma unroll
             for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -114,8 +113,11 @@ k_fp8_gemm_kslice(const Fp8TileArgs p) {
                     for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(t[e], f, acc[i][j][e]);
                 }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            cur = cur == NSTAGE - 1 ? 0 : cur + 1;
-        }
+        };
+        for (int s = 0; s < steps; s += NSTAGE)
+            static_for<NSTAGE>([&](auto uc) {
+                if (decltype(uc)::value == 0 || s + decltype(uc)::value < steps) step(uc, s + decltype(uc)::value);
+            });
         wait_vm<0>();
     }
     __syncthreads();
