@@ -19,10 +19,10 @@ __device__ __forceinline__ u32x4 buffer_of(const void* p, uint32_t bytes) {
     return u32x4{(uint32_t)a, (uint32_t)(a >> 32) & 0xFFFFu, bytes, 0x00027000u};
 }
 
-// 16 bytes a lane from a buffer, at a byte offset per lane plus a wave-uniform one, to LDS place lds + AT; bytes beyond the buffer's end
-// arrive as zeros.
-template <int AT> __device__ __forceinline__ void dma16_to(u32x4 rsrc, uint32_t voff, uint32_t soff, uint32_t lds) {
-    asm volatile("s_add_u32 m0, %3, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(voff), "s"(rsrc), "s"(soff), "s"(lds), "n"(AT) : "memory", "scc");
+// 16 bytes a lane from a buffer to LDS place lds + AT; dwords beyond the buffer's end arrive as zeros.  All of the offset is in the vector
+// register: the range check leaves a scalar offset out.
+template <int AT> __device__ __forceinline__ void dma16_to(u32x4 rsrc, uint32_t voff, uint32_t lds) {
+    asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "s"(lds), "n"(AT) : "memory", "scc");
 }
 
 // LDS swizzle of rows of 128 bytes of which 16 are read together, 16 bytes each: chunk c of row r sits at position c ^ swz16(r).

@@ -50,7 +50,7 @@ k_fp8_gemm_kslice(const Fp8TileArgs p) {
             constexpr int q = decltype(qc)::value, r = 8 * q, b = r - AR;
             const uint32_t row = (uint32_t)(r < AR ? m0 + r : n0 + (b < BO ? b : b - BO)) * (uint32_t)p.K;
             // the odd blocks' rows have the other half of the swizzles
-            dma16_to<decltype(stage)::value * STAGE + q * 1024>(r < AR ? x_buf : GATED && b >= BO ? u_buf : w_buf, (q & 1) ? at ^ 64 : at, row, lds0);
+            dma16_to<decltype(stage)::value * STAGE + q * 1024>(r < AR ? x_buf : GATED && b >= BO ? u_buf : w_buf, ((q & 1) ? at ^ 64 : at) + row, lds0);
         });
     };
     // scales of steps 4 g .. 4 g + 3: sixteen bytes of every token and block of channels, those beyond the end of the array as zeros
@@ -169,33 +169,16 @@ template <int AR, int BN, int NW, int NSTAGE, bool GATED> pme_status launch_ksli
     return hip_status(hipGetLastError());
 }
 
-template <bool GATED> pme_status launch_of(const Fp8GemmArgs& a, int id) {
-    if constexpr (!GATED) switch (id) {
-        case 0: return launch_kslice<8, 16, 8, 6, GATED>(a);
-        case 1: return launch_kslice<16, 16, 8, 4, GATED>(a);
+template <bool GATED> pme_status launch_of(const Fp8GemmArgs& a, int tile) {
+    if constexpr (!GATED) switch (tile) {
+        case 0: return launch_kslice<8, 16, 4, 5, GATED>(a);
+        case 1: return launch_kslice<16, 16, 4, 4, GATED>(a);
     }
-    switch (id) {
-        case 2: return launch_kslice<8, 32, 8, 3, GATED>(a);
-        case 3: return launch_kslice<16, 32, 8, 3, GATED>(a);
-        case 4: return launch_kslice<32, 32, 4, 4, GATED>(a);
-        case 5: return launch_kslice<8, 32, 4, 6, GATED>(a);
-        case 6: return launch_kslice<8, 32, 4, 3, GATED>(a);
-        case 7: return launch_kslice<16, 64, 4, 3, GATED>(a);
-        case 8: return launch_kslice<32, 64, 4, 3, GATED>(a);
-        case 9: return launch_kslice<16, 32, 4, 3, GATED>(a);
-        case 10: return launch_kslice<32, 32, 4, 2, GATED>(a);
-        case 11: return launch_kslice<32, 64, 4, 2, GATED>(a);
-        case 12: return launch_kslice<8, 64, 4, 2, GATED>(a);
-        case 13: return launch_kslice<8, 32, 2, 6, GATED>(a);
-        case 14: return launch_kslice<16, 32, 4, 2, GATED>(a);
-        case 15: return launch_kslice<8, 32, 4, 2, GATED>(a);
-        case 16: return launch_kslice<16, 64, 2, 3, GATED>(a);
-        case 17: return launch_kslice<32, 64, 2, 3, GATED>(a);
-        case 18: return launch_kslice<32, 32, 2, 3, GATED>(a);
-        case 19: return launch_kslice<48, 32, 4, 2, GATED>(a);
-        case 20: return launch_kslice<64, 32, 4, 2, GATED>(a);
-        case 21: return launch_kslice<64, 64, 2, 2, GATED>(a);
-        case 22: return launch_kslice<64, 64, 4, 2, GATED>(a);
+    switch (tile) {
+        case 2: return launch_kslice<8, 32, 4, 3, GATED>(a);
+        case 3: return launch_kslice<16, 32, 4, 2, GATED>(a);
+        case 4: return launch_kslice<32, 32, 4, 2, GATED>(a);
+        case 5: return launch_kslice<64, 32, 4, 2, GATED>(a);
     }
     return PME_ERR_UNSUPPORTED_PATH;
 }

@@ -149,8 +149,7 @@ struct Fp8GemmArgs {
 };
 pme_status launch_fp8_gemm_generic(const Fp8GemmArgs& a);
 pme_status launch_fp8_gemm_mfma(const Fp8GemmArgs& a);
-pme_status launch_fp8_gemm_decode(const Fp8GemmArgs& a);
-pme_status launch_fp8_gemm_kslice(const Fp8GemmArgs& a, int tile);
+pme_status launch_fp8_gemm_kslice(const Fp8GemmArgs& a, int tile);      // 0 .. 5: 8 x 16, 16 x 16, 8 x 32, 16 x 32, 32 x 32, 64 x 32 (the first two not gated)
 void set_fp8_tile_override(int id);
 
 // Lets `kern` be launched with up to `bytes` of dynamic LDS.  The attribute is set once per kernel and

@@ -72,6 +72,32 @@ def test_fp8_gemm_plan_argument_errors():
     assert f(1, 4, 256, 8, buf, 64) == OK and buf.value.startswith(b"k_fp8_")
 
 
+# tokens, features, channels, gated, the tile estimated fastest
+@pytest.mark.parametrize("T,K,N,gated,kernel", [
+    (1, 8192, 2048, False, "k_fp8_gemm_kslice<8, 16, "), (16, 14336, 4096, False, "k_fp8_gemm_kslice<16, 16, "), (8, 2048, 8192, True, "k_fp8_gemm_kslice<16, 32, "), (2, 4096, 2048, True, "k_fp8_gemm_kslice<8, 32, "),
+    (16, 4096, 14336, True, "k_fp8_gemm_kslice<16, 32, "), (64, 4096, 4096, False, "k_fp8_gemm_kslice<32, 32, "), (128, 4096, 4096, False, "k_fp8_gemm_kslice<64, 32, "),
+    (333, 4096, 4096, False, "k_fp8_gemm<64, 128, "), (517, 4096, 4096, False, "k_fp8_gemm<128, 128, "), (2048, 4096, 4096, False, "k_fp8_gemm<128, 256, "),
+    (4096, 14336, 4096, False, "k_fp8_gemm<256, 256, "), (1999, 4096, 14336, True, "k_fp8_gemm<256, 256, ")])
+def test_fp8_gemm_plan_by_fitted_times(T, K, N, gated, kernel):
+    assert pme.fp8_gemm_plan(T, K, N, gated=gated).startswith(kernel)
+
+
+def test_a_forced_fp8_tile_that_refuses_is_not_replaced():
+    f, buf = pme.lib().pme_fp8_gemm_plan, C.create_string_buffer(96)
+    try:
+        for tile, gated in ((201, 1), (202, 1), (214, 0), (299, 1)):
+            pme.set_gemm_tile(tile)
+            assert pme.fp8_gemm_plan(8, 512, 300, gated=bool(gated)).startswith("k_fp8_gemm_generic<")
+            pme.set_path(pme.PATH_MFMA)
+            assert f(gated, 8, 512, 300, buf, 96) == PATH
+            pme.set_path(pme.PATH_AUTO)
+        pme.set_gemm_tile(201)
+        assert pme.fp8_gemm_plan(8, 512, 300) == "k_fp8_gemm_kslice<8, 16, 4, 5, false>"
+    finally:
+        pme.set_gemm_tile(0)
+        pme.set_path(pme.PATH_AUTO)
+
+
 def test_binding_refuses_host_tensors_and_wrong_operands():
     x, w = torch.zeros(2, 130), torch.zeros(130)
     with pytest.raises(ValueError):

@@ -277,9 +277,10 @@ def test_fp8_gated_gemm(T, K, N):
         check_gated(y, ops)
 
 
-# every tile, forced: one K block, K blocks that fill neither a stage nor a group of four scales, several tiles with ragged ends
-TILES = [*range(201, 208), 240, 241, 242, 243, 245, 246]
-TILE_SHAPES = [(1, 128, 16), (40, 384, 72), (300, 640, 530), (257, 1152, 385), (96, 2432, 128)]
+# every tile, forced: one K block and fewer blocks than waves, K blocks that fill neither a stage nor a group of four scales, uneven shares
+# of K, rings filled several times, several tiles with ragged ends
+TILES = range(201, 214)
+TILE_SHAPES = [(1, 128, 16), (8, 384, 33), (40, 384, 72), (300, 640, 530), (257, 1152, 385), (96, 2432, 128), (7, 8320, 40), (33, 12416, 72), (16, 6144, 130)]
 
 
 @pytest.mark.parametrize("T,K,N", TILE_SHAPES)
@@ -288,42 +289,13 @@ def test_fp8_tiles(tile, T, K, N):
     ops = _operands(T, K, N, tile + T + K + N, mats=2)
     pme.set_path(pme.PATH_MFMA)
     pme.set_gemm_tile(tile)
-    y, z = pme.fp8_gemm(*ops[:4]), pme.fp8_gated_gemm(*ops)
-    torch.cuda.synchronize()
-    check_gemm(y, ops[:4])
-    check_gated(z, ops)
-
-
-# the weight-streaming kernel: channels by eight and by sixteen, odd numbers of K blocks, blocks for 4, 8 and 16 waves
-@pytest.mark.parametrize("T,K,N", [(1, 128, 1), (1, 384, 9), (8, 1152, 100), (7, 2176, 140), (8, 8320, 72), (3, 4224, 4104), (9, 384, 33), (16, 1152, 250), (15, 4224, 130),
-                                   (17, 384, 16), (32, 4224, 100), (31, 1280, 77)])
-def test_fp8_decode(T, K, N):
-    ops = _operands(T, K, N, T + K + N, mats=2)
-    pme.set_path(pme.PATH_MFMA)
-    pme.set_gemm_tile(208)
-    y, z = pme.fp8_gemm(*ops[:4]), pme.fp8_gated_gemm(*ops)
-    torch.cuda.synchronize()
-    check_gemm(y, ops[:4])
-    check_gated(z, ops)
-
-
-# waves that split K: fewer blocks than waves, uneven shares, several groups of scales a wave, the ring filled several times
-KSLICE = range(210, 233)
-
-
-@pytest.mark.parametrize("T,K,N", [(1, 128, 1), (8, 384, 33), (7, 8320, 40), (40, 1152, 140), (33, 12416, 72), (16, 6144, 130)])
-@pytest.mark.parametrize("tile", KSLICE)
-def test_fp8_kslice(tile, T, K, N):
-    ops = _operands(T, K, N, tile + T + K + N, mats=2)
-    pme.set_path(pme.PATH_MFMA)
-    pme.set_gemm_tile(tile)
-    if tile not in (210, 211):                        # tiles of 16 rows of weights are not gated
-        z = pme.fp8_gated_gemm(*ops)
-        torch.cuda.synchronize()
-        check_gated(z, ops)
     y = pme.fp8_gemm(*ops[:4])
     torch.cuda.synchronize()
     check_gemm(y, ops[:4])
+    if tile > 202:                                    # tiles of 16 rows of weights have no room for two matrices
+        z = pme.fp8_gated_gemm(*ops)
+        torch.cuda.synchronize()
+        check_gated(z, ops)
 
 
 def test_products_write_their_columns_only():
