@@ -324,13 +324,23 @@ FP8_BLOCK = 128
 _FP8 = torch.float8_e4m3fn
 
 
-def _here(*tensors) -> int:
-    """The device all of `tensors` are on, which has to be the current one (the launches go to its current stream)."""
-    dev = torch.cuda.current_device() if tensors[0].is_cuda else -1
+def _stream_here(*tensors) -> int:
+    """The current stream, of the device that all of `tensors` have to be on."""
+    dev = torch.cuda.current_device() if tensors[0].is_cuda else -2
     for t in tensors:
-        if not t.is_cuda or t.get_device() != dev:
+        if t.get_device() != dev:
             raise ValueError("every operand must be a tensor of the current device")
-    return dev
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _matrix(x: torch.Tensor):
+    """As _rows, with fewer calls (the host's share of the smallest calls is most of them)."""
+    if x.dim() != 2:
+        raise ValueError("a [rows, d] matrix is required")
+    (rows, d), (ld, unit) = x.shape, x.stride()
+    if unit != 1:
+        raise ValueError("a matrix must have unit stride along its rows")
+    return rows, d, ld if rows > 1 or ld > d else d
 
 
 def _codes_out(q, s, rows: int, srows: int, d: int, device):
@@ -350,54 +360,56 @@ def rmsnorm_quant_fp8(x: torch.Tensor, weight: torch.Tensor, eps: float, residua
                       h: torch.Tensor | None = None, qx: torch.Tensor | None = None, sx: torch.Tensor | None = None):
     """Codes and scales of the root-mean-square norm of x, or of h = x + residual when a residual is given
     -> (qx, sx), or (qx, sx, h).  h may be x or residual itself."""
-    T, d, ldx = _rows(x)
-    xt, wt = _dtype_code(x), _dtype_code(weight)
-    if weight.dim() != 1 or weight.shape[0] != d or not weight.is_contiguous():
+    T, d, ldx = _matrix(x)
+    dtype = x.dtype
+    xt = _dtype_code(x)
+    wt = xt if weight.dtype == dtype else _dtype_code(weight)
+    if weight.shape != (d,) or not weight.is_contiguous():
         raise ValueError("weight must be a contiguous [d] tensor")
+    qx, sx = _codes_out(qx, sx, T, T, d, x.device)
     if residual is None:
         if h is not None:
             raise ValueError("h is the sum with a residual: give both or neither")
-        qx, sx = _codes_out(qx, sx, T, T, d, x.device)
-        _here(x, weight, qx, sx)
+        stream = _stream_here(x, weight, qx, sx)
         _check(lib().pme_rmsnorm_quant_fp8(x.data_ptr(), xt, T, d, ldx, None, 0, None, 0, weight.data_ptr(), wt, eps,
-                                           qx.data_ptr(), sx.data_ptr(), _stream()), "pme_rmsnorm_quant_fp8")
+                                           qx.data_ptr(), sx.data_ptr(), stream), "pme_rmsnorm_quant_fp8")
         return qx, sx
     if h is None:
-        h = torch.empty((T, d), dtype=x.dtype, device=x.device)
-    if residual.dtype != x.dtype or h.dtype != x.dtype or residual.shape != x.shape or h.shape != x.shape:
+        h = torch.empty((T, d), dtype=dtype, device=x.device)
+    Tr, dr, ldr = _matrix(residual)
+    Th, dh, ldh = _matrix(h)
+    if residual.dtype != dtype or h.dtype != dtype or Tr != T or Th != T or dr != d or dh != d:
         raise ValueError("residual and h must have x's shape and type")
-    ldr, ldh = _rows(residual)[2], _rows(h)[2]
-    qx, sx = _codes_out(qx, sx, T, T, d, x.device)
-    _here(x, residual, h, weight, qx, sx)
+    stream = _stream_here(x, residual, h, weight, qx, sx)
     _check(lib().pme_rmsnorm_quant_fp8(x.data_ptr(), xt, T, d, ldx, residual.data_ptr(), ldr, h.data_ptr(), ldh,
-                                       weight.data_ptr(), wt, eps, qx.data_ptr(), sx.data_ptr(), _stream()),
+                                       weight.data_ptr(), wt, eps, qx.data_ptr(), sx.data_ptr(), stream),
            "pme_rmsnorm_quant_fp8")
     return qx, sx, h
 
 
 def quant_fp8(x: torch.Tensor, qx: torch.Tensor | None = None, sx: torch.Tensor | None = None):
     """Codes and scales of activations [T, d], a scale for each token and group of 128 features -> (qx, sx)."""
-    T, d, ldx = _rows(x)
+    T, d, ldx = _matrix(x)
     xt = _dtype_code(x)
     qx, sx = _codes_out(qx, sx, T, T, d, x.device)
-    _here(x, qx, sx)
-    _check(lib().pme_quant_fp8(x.data_ptr(), xt, T, d, ldx, qx.data_ptr(), sx.data_ptr(), _stream()), "pme_quant_fp8")
+    stream = _stream_here(x, qx, sx)
+    _check(lib().pme_quant_fp8(x.data_ptr(), xt, T, d, ldx, qx.data_ptr(), sx.data_ptr(), stream), "pme_quant_fp8")
     return qx, sx
 
 
 def quantize_weights_fp8(wt: torch.Tensor, qw: torch.Tensor | None = None, sw: torch.Tensor | None = None):
     """Codes and scales of weights [N, d] (torch Linear layout), a scale for each block of 128 x 128 -> (qw, sw)."""
-    N, d, ldw = _rows(wt)
+    N, d, ldw = _matrix(wt)
     code = _dtype_code(wt)
     qw, sw = _codes_out(qw, sw, N, (N + FP8_BLOCK - 1) // FP8_BLOCK, d, wt.device)
-    _here(wt, qw, sw)
-    _check(lib().pme_quantize_weights_fp8(wt.data_ptr(), code, N, d, ldw, qw.data_ptr(), sw.data_ptr(), _stream()),
+    stream = _stream_here(wt, qw, sw)
+    _check(lib().pme_quantize_weights_fp8(wt.data_ptr(), code, N, d, ldw, qw.data_ptr(), sw.data_ptr(), stream),
            "pme_quantize_weights_fp8")
     return qw, sw
 
 
 def _fp8_operand(q, s, what: str, per: int):
-    if q.dim() != 2 or q.dtype != _FP8 or not q.is_contiguous() or q.shape[1] % FP8_BLOCK:
+    if q.dtype != _FP8 or q.dim() != 2 or not q.is_contiguous() or q.shape[1] % FP8_BLOCK:
         raise ValueError(f"q{what} must be a contiguous float8_e4m3fn tensor with rows of whole groups of 128")
     rows, K = q.shape
     if s.dtype != torch.float32 or s.shape != ((rows + per - 1) // per, K // FP8_BLOCK) or not s.is_contiguous():
@@ -408,9 +420,12 @@ def _fp8_operand(q, s, what: str, per: int):
 def _fp8_out(y, T: int, N: int, device):
     if y is None:
         return torch.empty((T, N), dtype=torch.bfloat16, device=device), N
-    if y.dtype != torch.bfloat16 or y.shape != (T, N) or (N > 1 and y.stride(1) != 1):
-        raise ValueError(f"y must be a bfloat16 [{T}, {N}] tensor with unit stride along its rows")
-    return y, y.stride(0) if T > 1 else max(y.stride(0), N)
+    if y.dtype != torch.bfloat16 or y.shape != (T, N):
+        raise ValueError(f"y must be a bfloat16 [{T}, {N}] tensor")
+    ldy, unit = y.stride()
+    if unit != 1 and N > 1:
+        raise ValueError("y must have unit stride along its rows")
+    return y, ldy if T > 1 or ldy > N else N
 
 
 def fp8_gemm(qx, sx, qw, sw, y: torch.Tensor | None = None) -> torch.Tensor:
@@ -420,8 +435,8 @@ def fp8_gemm(qx, sx, qw, sw, y: torch.Tensor | None = None) -> torch.Tensor:
     if Kw != K:
         raise ValueError("qx and qw disagree on K")
     y, ldy = _fp8_out(y, T, N, qx.device)
-    _here(qx, sx, qw, sw, y)
-    _check(lib().pme_fp8_gemm(qx.data_ptr(), sx.data_ptr(), qw.data_ptr(), sw.data_ptr(), T, K, N, y.data_ptr(), ldy, _stream()),
+    stream = _stream_here(qx, sx, qw, sw, y)
+    _check(lib().pme_fp8_gemm(qx.data_ptr(), sx.data_ptr(), qw.data_ptr(), sw.data_ptr(), T, K, N, y.data_ptr(), ldy, stream),
            "pme_fp8_gemm")
     return y
 
@@ -433,9 +448,9 @@ def fp8_gated_gemm(qx, sx, qg, sg, qu, su, y: torch.Tensor | None = None) -> tor
     if _fp8_operand(qu, su, "u", FP8_BLOCK) != (N, K) or Kg != K:
         raise ValueError("qx, qg and qu disagree on K, or qg and qu on N")
     y, ldy = _fp8_out(y, T, N, qx.device)
-    _here(qx, sx, qg, sg, qu, su, y)
+    stream = _stream_here(qx, sx, qg, sg, qu, su, y)
     _check(lib().pme_fp8_gated_gemm(qx.data_ptr(), sx.data_ptr(), qg.data_ptr(), sg.data_ptr(), qu.data_ptr(), su.data_ptr(),
-                                    T, K, N, y.data_ptr(), ldy, _stream()), "pme_fp8_gated_gemm")
+                                    T, K, N, y.data_ptr(), ldy, stream), "pme_fp8_gated_gemm")
     return y
 
 
