@@ -38,7 +38,7 @@ struct Fp8TileArgs {
     int T, N, K;
     uint16_t* y;
     int64_t ldo;
-    int tiles_m, tiles_n, xcd_gm, vec_store;
+    int tiles_m, tiles_n, xcd_gm;
 };
 
 }  // namespace

@@ -352,19 +352,17 @@ k_fp8_gemm(const Fp8TileArgs p) {
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         const int tbase = m0 + wm * WM + 16 * i, nbase = n0 + wn * WO;
-        if (p.vec_store) {
-            constexpr int CPS = WO / 8;
+        constexpr int CPS = WO / 8;
 #pragma unroll
-            for (int c = lane; c < 16 * CPS; c += 64) {
-                const int row = c / CPS, col = (c % CPS) * 8;
-                const u32x4 v = *reinterpret_cast<const u32x4*>(slab + row * (WO * 2) + col * 2);
-                if (tbase + row < p.T && nbase + col < p.N) *reinterpret_cast<u32x4*>(p.y + (int64_t)(tbase + row) * p.ldo + nbase + col) = v;
-            }
-        } else {
-            for (int c = lane; c < 16 * WO; c += 64) {
-                const int row = c / WO, col = c % WO;
-                if (tbase + row < p.T && nbase + col < p.N)
-                    p.y[(int64_t)(tbase + row) * p.ldo + nbase + col] = *reinterpret_cast<const uint16_t*>(slab + row * (WO * 2) + col * 2);
+        for (int c = lane; c < 16 * CPS; c += 64) {
+            const int row = c / CPS, col = (c % CPS) * 8;
+            const uint16_t* from = reinterpret_cast<const uint16_t*>(slab + row * (WO * 2) + col * 2);
+            uint16_t* to = p.y + (int64_t)(tbase + row) * p.ldo + nbase + col;
+            if (tbase + row < p.T) {
+                // 16 bytes wherever they lie: the memory system takes wide accesses at any address
+                if (nbase + col + 8 <= p.N) __builtin_memcpy(to, from, 16);
+                else
+                    for (int e = 0; nbase + col + e < p.N; ++e) to[e] = from[e];
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -391,9 +389,8 @@ template <int BM, int BN, int WGM, int WGN, int KS, int NSTAGE, bool AHEAD, bool
     auto kern = k_fp8_gemm<BM, BN, WGM, WGN, KS, NSTAGE, AHEAD, GATED>;
     static std::atomic<uint32_t> done;
     if (allow_dynamic_lds(kern, lds, done) != PME_OK) return PME_ERR_HIP;
-    const int vec = (a.N % 8 == 0 && a.ldy % 8 == 0 && (reinterpret_cast<uintptr_t>(a.y) & 15) == 0) ? 1 : 0;
     const Fp8TileArgs p{a.qx, a.sx, a.qw, a.sw, a.qu, a.su, (int)a.T, (int)a.N, (int)a.K, static_cast<uint16_t*>(a.y), a.ldy,
-                        tiles_m, tiles_n, xcd_grid_m(tiles_m, tiles_n, BM, BN), vec};
+                        tiles_m, tiles_n, xcd_grid_m(tiles_m, tiles_n, BM, BN)};
     hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * WGM * WGN * KS), lds, a.stream, p);
     return hip_status(hipGetLastError());
 }

@@ -164,7 +164,7 @@ template <int AR, int BN, int NW, int NSTAGE, bool GATED> pme_status launch_ksli
     static std::atomic<uint32_t> done;
     if (allow_dynamic_lds(kern, lds, done) != PME_OK) return PME_ERR_HIP;
     const Fp8TileArgs p{a.qx, a.sx, a.qw, a.sw, a.qu, a.su, (int)a.T, (int)a.N, (int)a.K, static_cast<uint16_t*>(a.y), a.ldy,
-                        tiles_m, tiles_n, xcd_grid_m(tiles_m, tiles_n, AR, BN), 0};
+                        tiles_m, tiles_n, xcd_grid_m(tiles_m, tiles_n, AR, BN)};
     hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * NW), lds, a.stream, p);
     return hip_status(hipGetLastError());
 }
