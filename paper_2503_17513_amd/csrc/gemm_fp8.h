@@ -38,8 +38,25 @@ struct Fp8TileArgs {
     int T, N, K;
     uint16_t* y;
     int64_t ldo;
-    int tiles_m, tiles_n, xcd_gm;
+    int tiles_m, tiles_n, band;
 };
+
+// Workgroup -> output tile.  Workgroups are dealt round-robin to the 8 XCDs, each with an L2 of its own: XCD x takes a contiguous share of
+// the tiles in an order that walks bands of `band` rows of tiles column by column, so that what it works on at a time is a block of about
+// as many rows of tokens as of weights.
+__device__ __forceinline__ void fp8_tile(int wg, int tiles_m, int tiles_n, int band, int& tm, int& tn) {
+    const int n = tiles_m * tiles_n, x = wg & 7, t = x * (n >> 3) + min(x, n & 7) + (wg >> 3);
+    const int b = t / (band * tiles_n), first = b * band, rows = min(band, tiles_m - first), r = t - first * tiles_n;
+    tm = first + r % rows;
+    tn = r / rows;
+}
+// The band of tiles of `rows` tokens and `weights` weights, `resident` of them on a compute unit at a time.
+inline int fp8_band(int tiles_m, int tiles_n, int rows, int weights, int resident) {
+    const int most = tiles_m * tiles_n / 8 + 1, c = most < 32 * resident ? most : 32 * resident;
+    int band = 1;
+    while (band < tiles_m && (band + 1) * band * rows <= c * weights) ++band;      // band * rows <= c / band * weights, to the nearer side
+    return band;
+}
 
 }  // namespace
 }  // namespace pme

@@ -72,7 +72,7 @@ k_fp8_gemm(const Fp8TileArgs p) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int w = wave % NWW, ks = wave / NWW, wm = w / WGN, wn = w % WGN;
     int tm, tn;
-    xcd_tile((int)blockIdx.x, p.tiles_m, p.tiles_n, p.xcd_gm, tm, tn);
+    fp8_tile((int)blockIdx.x, p.tiles_m, p.tiles_n, p.band, tm, tn);
     const int m0 = tm * BM, n0 = tn * BO, groups = p.K / 128, KT = (groups + KS - 1) / KS;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(PME_AS3 unsigned char*)smem;
 
@@ -390,7 +390,7 @@ template <int BM, int BN, int WGM, int WGN, int KS, int NSTAGE, bool AHEAD, bool
     static std::atomic<uint32_t> done;
     if (allow_dynamic_lds(kern, lds, done) != PME_OK) return PME_ERR_HIP;
     const Fp8TileArgs p{a.qx, a.sx, a.qw, a.sw, a.qu, a.su, (int)a.T, (int)a.N, (int)a.K, static_cast<uint16_t*>(a.y), a.ldy,
-                        tiles_m, tiles_n, xcd_grid_m(tiles_m, tiles_n, BM, BN)};
+                        tiles_m, tiles_n, fp8_band(tiles_m, tiles_n, BM, BN, 160 * 1024 / lds)};
     hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * WGM * WGN * KS), lds, a.stream, p);
     return hip_status(hipGetLastError());
 }

@@ -33,7 +33,7 @@ k_fp8_gemm_kslice(const Fp8TileArgs p) {
     extern __shared__ __align__(1024) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int tm, tn;
-    xcd_tile((int)blockIdx.x, p.tiles_m, p.tiles_n, p.xcd_gm, tm, tn);
+    fp8_tile((int)blockIdx.x, p.tiles_m, p.tiles_n, p.band, tm, tn);
     const int m0 = tm * AR, n0 = tn * BO, groups = p.K / 128;
     const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)wave * groups / NW));
     const int steps = __builtin_amdgcn_readfirstlane((int)((int64_t)(wave + 1) * groups / NW) - first);
@@ -164,7 +164,7 @@ template <int AR, int BN, int NW, int NSTAGE, bool GATED> pme_status launch_ksli
     static std::atomic<uint32_t> done;
     if (allow_dynamic_lds(kern, lds, done) != PME_OK) return PME_ERR_HIP;
     const Fp8TileArgs p{a.qx, a.sx, a.qw, a.sw, a.qu, a.su, (int)a.T, (int)a.N, (int)a.K, static_cast<uint16_t*>(a.y), a.ldy,
-                        tiles_m, tiles_n, xcd_grid_m(tiles_m, tiles_n, AR, BN)};
+                        tiles_m, tiles_n, fp8_band(tiles_m, tiles_n, AR, BN, 160 * 1024 / lds)};
     hipLaunchKernelGGL(kern, dim3((unsigned)(tiles_m * tiles_n)), dim3(64 * NW), lds, a.stream, p);
     return hip_status(hipGetLastError());
 }
