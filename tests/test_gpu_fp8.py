@@ -298,6 +298,21 @@ def test_fp8_tiles(tile, T, K, N):
         check_gated(z, ops)
 
 
+@pytest.mark.parametrize("T,K,N,first,gated", [(905, 768, 4141, 4096, True), (2845, 768, 2817, 2816, False), (226, 2048, 8444, 8192, True)])
+def test_whole_rounds_and_the_channels_behind_them(T, K, N, first, gated):
+    """Shapes whose last channels another tile computes: the first block of 128 channels, the last one before them, and themselves."""
+    ops = _operands(T, K, N, T + N, mats=2 if gated else 1)
+    y = (pme.fp8_gated_gemm if gated else pme.fp8_gemm)(*ops)
+    torch.cuda.synchronize()
+    assert not bool(torch.isnan(y).any())
+    blocks = [0, first // 128 - 1, *range(first // 128, (N + 127) // 128)]
+    rows = torch.cat([torch.arange(128 * b, min(128 * b + 128, N)) for b in blocks]).cuda()
+    part = ops[:2]
+    for q, s in zip(ops[2::2], ops[3::2]):
+        part += [q.view(torch.uint8)[rows].view(torch.float8_e4m3fn), s[torch.tensor(blocks).cuda()]]
+    (check_gated if gated else check_gemm)(y[:, rows], part)
+
+
 def test_products_write_their_columns_only():
     for T, K, N in ((5, 256, 67), (150, 512, 333)):
         ops = _operands(T, K, N, 9, mats=2)
