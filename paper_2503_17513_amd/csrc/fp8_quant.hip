@@ -129,25 +129,18 @@ __device__ __forceinline__ void quantize_chunk(const float (&v)[8], int c, uint8
 
 template <bool F32> __device__ __forceinline__ const elem_t<F32>* row_of(const void* p, int64_t row, int64_t ld) { return static_cast<const elem_t<F32>*>(p) + row * ld; }
 
-// ---- activations as they are: a workgroup takes 256 NV chunks of a row.
-template <bool F32, int NV>
+// ---- activations as they are: a workgroup takes 256 chunks of a row (two or four chunks a lane: 0 to 10 % and 5 to 60 % slower).
+template <bool F32>
 __global__ void __launch_bounds__(256)
 k_quant_fp8(const void* __restrict__ x, int64_t rows, int d, int64_t ldx, int groups, uint8_t* __restrict__ q, float* __restrict__ s) {
-    const int c0 = (int)blockIdx.x * (256 * NV) + (int)threadIdx.x;
+    const int c = (int)(blockIdx.x * 256 + threadIdx.x);
+    if (c >= 16 * groups) return;                   // whole groups: the lanes of one go together
     for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
-        const elem_t<F32>* xr = row_of<F32>(x, row, ldx);
-        Chunk<F32> k[NV];
+        const Chunk<F32> k = load_chunk<F32>(row_of<F32>(x, row, ldx), c, d);
+        float v[8];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) k[i] = load_chunk<F32>(xr, c0 + 256 * i, d);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (c0 + 256 * i < 16 * groups) {       // whole groups: the lanes of one go together
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = k[i].get(e);
-                quantize_chunk(v, c0 + 256 * i, q + row * groups * kGroup, s + row * groups);
-            }
-        }
+        for (int e = 0; e < 8; ++e) v[e] = k.get(e);
+        quantize_chunk(v, c, q + row * groups * kGroup, s + row * groups);
     }
 }
 
@@ -161,6 +154,7 @@ k_rmsnorm_quant_fp8(const NormQuantArgs a) {
     const int l = ONE_WAVE ? lane : (int)threadIdx.x, L = ONE_WAVE ? 64 : (int)blockDim.x;
     const int d = (int)a.d, groups = (int)((a.d + kGroup - 1) / kGroup), all = 16 * groups;
     constexpr int N = NV ? NV : 1;
+    constexpr bool EARLY = NV > 0 && !(F32 && WF32 && NV == 4);      // the weights' registers fit too
     const int rounds = NV ? 1 : (all + L - 1) / L;
     int parity = 0;
     for (int64_t row = ONE_WAVE ? (int64_t)blockIdx.x * waves + wave : (int64_t)blockIdx.x; row < a.T; row += ONE_WAVE ? (int64_t)gridDim.x * waves : (int64_t)gridDim.x, parity ^= 1) {
@@ -193,7 +187,7 @@ k_rmsnorm_quant_fp8(const NormQuantArgs a) {
                 k[i] = load_chunk<F32>(xr, c0 + i * L, d);
                 if constexpr (RES) t[i] = load_chunk<F32>(rr, c0 + i * L, d);
             }
-            if constexpr (NV > 0) {      // ahead of the sum, so that the second half waits for nothing
+            if constexpr (EARLY) {       // ahead of the sum, so that the second half waits for nothing
 #pragma unroll
                 for (int i = 0; i < N; ++i) w[i] = load_chunk<WF32>(wr, c0 + i * L, d);
             }
@@ -250,10 +244,8 @@ k_rmsnorm_quant_fp8(const NormQuantArgs a) {
             for (int i = 0; i < N; ++i) {
                 const int c = r * L + l + i * L;
                 if (c >= all) continue;         // whole groups: the lanes of one go together
-                if constexpr (NV == 0) {
-                    k[i] = load_chunk<F32>(RES ? hr : xr, c, d);
-                    w[i] = load_chunk<WF32>(wr, c, d);
-                }
+                if constexpr (NV == 0) k[i] = load_chunk<F32>(RES ? hr : xr, c, d);
+                if constexpr (!EARLY) w[i] = load_chunk<WF32>(wr, c, d);
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = k[i].get(e) * pre * rms * w[i].get(e);
@@ -310,11 +302,16 @@ template <bool F32, bool WF32, bool RES, int NV, bool ONE_WAVE> pme_status launc
     return hip_status(hipGetLastError());
 }
 
+// A wave for rows of at most 512; otherwise the workgroup that holds the row with few chunks a lane, which have less to wait for one after
+// the other (us, one / two / four chunks, norm with a residual in bf16: 1 x 2048 3.0 / 3.4 / 4.1, 512 x 4096 5.4 / 5.5 / 6.5, 4096 x 8192 47 / 44 / 45);
+// rows of more than 16384 in bf16 four from 512 on, where fewer and lighter workgroups share a compute unit better (4096 x 14336 - / 87 / 80; in
+// fp32, whose row takes twice the registers, - / 163 / 186).
 template <bool F32, bool WF32, bool RES> pme_status norm_of(const NormQuantArgs& a) {
     const int64_t least = ((a.d + kGroup - 1) / kGroup * 16 + 63) / 64;      // waves with one chunk a lane
     if (least > 64) return launch_norm<F32, WF32, RES, 0, false>(a, 16);
-    if (a.T > 512 && least <= 4) return launch_norm<F32, WF32, RES, 4, true>(a, 4);
-    const int nv = a.T > 512 ? 4 : least <= 16 ? 1 : least <= 32 ? 2 : 4, waves = (int)((least + nv - 1) / nv);
+    if (least == 1) return launch_norm<F32, WF32, RES, 1, true>(a, 4);
+    const bool many = !F32 && a.T >= (least > 16 ? 512 : 2048);
+    const int nv = least > 32 || (least > 16 && many) ? 4 : least > 8 || (least >= 4 && many) ? 2 : 1, waves = (int)((least + nv - 1) / nv);
     if (nv == 1) return launch_norm<F32, WF32, RES, 1, false>(a, waves);
     if (nv == 2) return launch_norm<F32, WF32, RES, 2, false>(a, waves);
     return launch_norm<F32, WF32, RES, 4, false>(a, waves);
@@ -323,14 +320,10 @@ template <bool F32, bool WF32, bool RES> pme_status norm_of(const NormQuantArgs&
 template <bool F32, bool WF32> pme_status norm_of(const NormQuantArgs& a) { return a.residual ? norm_of<F32, WF32, true>(a) : norm_of<F32, WF32, false>(a); }
 
 template <bool F32> pme_status quant_of(const QuantArgs& a) {
-    const int64_t groups = (a.d + kGroup - 1) / kGroup, chunks = 16 * groups;
-    auto go = [&](auto nv) {
-        constexpr int NV = decltype(nv)::value;
-        const dim3 grid((unsigned)((chunks + 256 * NV - 1) / (256 * NV)), (unsigned)std::min(a.rows, kMostRows));
-        hipLaunchKernelGGL((k_quant_fp8<F32, NV>), grid, dim3(256), 0, a.stream, a.x, a.rows, (int)a.d, a.ldx, (int)groups, a.q, a.s);
-        return hip_status(hipGetLastError());
-    };
-    return a.rows * chunks <= 256 * 2048 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 2>{});
+    const int64_t groups = (a.d + kGroup - 1) / kGroup;
+    const dim3 grid((unsigned)((16 * groups + 255) / 256), (unsigned)std::min(a.rows, kMostRows));
+    hipLaunchKernelGGL((k_quant_fp8<F32>), grid, dim3(256), 0, a.stream, a.x, a.rows, (int)a.d, a.ldx, (int)groups, a.q, a.s);
+    return hip_status(hipGetLastError());
 }
 
 }  // namespace

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2503_17513_amd as pme
+from test_abi_host import _kernel_metadata
 
 OK, NULL, SHAPE, ORDER, ALIGN, WORKSPACE, DTYPE, HIP, PATH, COLD = range(10)
 FAKE = 0x10000   # a non-null, 64 KiB aligned address that is never dereferenced: every call below fails validation
@@ -96,6 +97,13 @@ def test_a_forced_fp8_tile_that_refuses_is_not_replaced():
     finally:
         pme.set_gemm_tile(0)
         pme.set_path(pme.PATH_AUTO)
+
+
+def test_fp8_kernels_use_no_scratch():
+    # accumulators, fragments and rows stay in registers
+    kernels = [k for k in _kernel_metadata() if any(n in k[".name"] for n in ("k_fp8_gemm", "_quant_fp8", "k_quantize_weights_fp8", "Fp8TileArgs", "NormQuantArgs"))]
+    assert len(kernels) >= 2 * 13 - 2 + 2 + 2 * 2 + 8 * 5
+    assert not [k[".name"] for k in kernels if k[".private_segment_fixed_size"] or k[".vgpr_spill_count"]]
 
 
 def test_binding_refuses_host_tensors_and_wrong_operands():
