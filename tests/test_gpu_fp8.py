@@ -313,6 +313,33 @@ def test_whole_rounds_and_the_channels_behind_them(T, K, N, first, gated):
     (check_gated if gated else check_gemm)(y[:, rows], part)
 
 
+def test_operands_beyond_4_gib():
+    """Codes of more than 2^32 bytes, as tokens and as weights: rows on both sides of the place where a launch's offsets end, and the last one."""
+    K, rows = 14336, 300032
+    cut = ((1 << 32) - 1) // K // 256 * 256
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(7)
+    big = torch.randint(0, 0x78, (rows, K), dtype=torch.uint8, device="cuda", generator=gen)
+    big[:, ::2] |= 0x80
+    big = big.view(torch.float8_e4m3fn)
+    sx = torch.rand((rows, K // 128), device="cuda", generator=gen) * 1e-3
+    sw = torch.rand(((rows + 127) // 128, K // 128), device="cuda", generator=gen) * 1e-3
+    qs, ss = _operands(40, K, 72, 11)[2:]                                         # 72 channels
+    qt, st = _operands(5, K, 8, 12)[:2]                                           # 5 tokens
+    at = torch.tensor([0, 127, cut - 1, cut, cut + 130, rows - 1], device="cuda")
+    pick = big.view(torch.uint8)[at].view(torch.float8_e4m3fn)
+    y = pme.fp8_gemm(big, sx, qs, ss)
+    torch.cuda.synchronize()
+    check_gemm(y[at], [pick, sx[at], qs, ss])
+    y = pme.fp8_gemm(qt, st, big, sw)
+    z = pme.fp8_gated_gemm(qt, st, big, sw, big, sw)
+    torch.cuda.synchronize()
+    for i, row in enumerate(at.tolist()):
+        one = [pick[i:i + 1], sw[row // 128:row // 128 + 1]]
+        check_gemm(y[:, row:row + 1], [qt, st, *one])
+        check_gated(z[:, row:row + 1], [qt, st, *one, *one])
+
+
 def test_products_write_their_columns_only():
     for T, K, N in ((5, 256, 67), (150, 512, 333)):
         ops = _operands(T, K, N, 9, mats=2)
