@@ -152,13 +152,13 @@ k_fp8_gemm(const Fp8TileArgs p) {
     };
     auto products = [&](const Scales& s, int kt) {
         Products r;
-        // a slice of K that has no block left in the last step works on its last block again, with a scale of zero
+        // a slice of K that has no block left in the last step works on its last block again, with a factor of zero (the scales read for it
+        // are the next token's, and may be anything)
         const bool live = KS == 1 || kt * KS + ks < groups;
-        const float sw = live ? s.w : 0.f, su = GATED && live ? s.u : 0.f;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            r.w[i] = s.x[i] * sw;
-            if constexpr (GATED) r.u[i] = s.x[i] * su;
+            r.w[i] = live ? s.x[i] * s.w : 0.f;
+            if constexpr (GATED) r.u[i] = live ? s.x[i] * s.u : 0.f;
         }
         return r;
     };

@@ -363,6 +363,30 @@ def test_nan_codes_reach_their_rows_only():
     assert torch.equal(y[:7], clean[:7]) and torch.equal(y[8:], clean[8:])
 
 
+@pytest.mark.parametrize("tile", TILES)
+def test_scales_that_are_not_finite_reach_their_rows_and_channels_only(tile):
+    """Blocks of K that fill no group of four scales and no whole step of the slices of K: the scales that follow a row's in memory are its neighbour's."""
+    for K in (128, 256, 384, 640, 1152, 1408):
+        ops = _operands(72, K, 300, 5, mats=2)
+        pme.set_path(pme.PATH_MFMA)
+        pme.set_gemm_tile(tile)
+        for f, o in ((pme.fp8_gemm, ops[:4]), (pme.fp8_gated_gemm, ops)):
+            if tile < 203 and f is pme.fp8_gated_gemm:
+                continue
+            clean = f(*o)
+            sx, sw = ops[1].clone(), ops[3].clone()
+            sx[7, 0], sx[40, -1], sx[41], sx[71, 0] = float("nan"), float("inf"), float("nan"), float("nan")
+            sw[1, 0] = float("nan")
+            y = f(o[0], sx, o[2], sw, *o[4:])
+            torch.cuda.synchronize()
+            bad = torch.zeros_like(y, dtype=torch.bool)
+            bad[[7, 41, 71]] = True
+            bad[:, 128:256] = True
+            assert bool(torch.isnan(y[bad]).all())
+            bad[40] = True                                # infinite, or NaN where infinities cancel
+            assert torch.equal(y[~bad], clean[~bad])
+
+
 # ---- together
 
 def _block(seed, T=70, d=640, f=704, f_e=768):
