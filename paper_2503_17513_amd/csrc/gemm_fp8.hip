@@ -207,15 +207,15 @@ k_fp8_gemm(const Fp8TileArgs p) {
     constexpr std::integral_constant<int, 0> first{};
     Scales s;
     if constexpr (AHEAD) {
-        // Every operand of a step is in registers when the step begins, and is replaced by the next one's as it is used: a step's LDS
-        // reads have the whole of the step before to arrive in, and nothing waits for the last of them at the barrier.
-        i32x8 a[2][FM], b[FN];
+        // Every operand of a step is in registers when the step begins, while the next one's are read into others: a step's LDS reads
+        // have the whole of the step before to arrive in, and nothing waits for the last of them at the barrier.
+        i32x8 a[2][FM], b[2][FN];
         static_for<DEPTH + 1>([&](auto st) { static_for<CH>([&](auto qc) { issue_codes(st, qc, decltype(st)::value); }); });
         wait_vm<DEPTH * CH>();
         lds_barrier();
         load_scales(s, 0);
         static_for<FM>([&](auto ic) { a[0][decltype(ic)::value] = load_a(first, ic); });
-        static_for<FN>([&](auto jc) { b[decltype(jc)::value] = load_b(first, jc); });
+        static_for<FN>([&](auto jc) { b[0][decltype(jc)::value] = load_b(first, jc); });
         auto step = [&](auto uc, int kt) {
             constexpr int u = decltype(uc)::value;
             constexpr std::integral_constant<int, (u + 1) % NSTAGE> nxt{};
@@ -228,7 +228,6 @@ k_fp8_gemm(const Fp8TileArgs p) {
             if (kt > 0 && kt % GS == 0) issue_scales(kt / GS + 1);
             now = products(s, kt);
             load_scales(s, kt + 1);
-            static_for<FM>([&](auto ic) { a[(u + 1) & 1][decltype(ic)::value] = load_a(nxt, ic); });
             static_for<FN>([&](auto jc) {
                 constexpr int j = decltype(jc)::value;
                 static_for<CH>([&](auto qc) {
@@ -238,8 +237,16 @@ k_fp8_gemm(const Fp8TileArgs p) {
                     constexpr std::integral_constant<int, j * FM + decltype(ic)::value> m{};
                     __builtin_amdgcn_sched_barrier(0);
                     if constexpr (m < 3) add_behind(before, now, m);
-                    multiply(m, b[j], a[u & 1][decltype(ic)::value]);
-                    if constexpr (decltype(ic)::value == FM - 1) b[j] = load_b(nxt, jc);
+                    multiply(m, b[u & 1][j], a[u & 1][decltype(ic)::value]);
+                    // the next step's fragments in the order of their use, evenly: 5 to 7 % of 128 x 128 over all of them first
+                    static_for<FM + FN>([&](auto lc) {
+                        constexpr int l = decltype(lc)::value;
+                        if constexpr (l * FM * FN / (FM + FN) == m) {
+                            if constexpr (l == 0) b[(u + 1) & 1][0] = load_b(nxt, first);
+                            else if constexpr (l <= FM) a[(u + 1) & 1][l - 1] = load_a(nxt, std::integral_constant<int, l - 1>{});
+                            else b[(u + 1) & 1][l - FM] = load_b(nxt, std::integral_constant<int, l - FM>{});
+                        }
+                    });
                     if constexpr (m >= 3) add_behind(before, now, m);
                 });
             });
