@@ -88,6 +88,8 @@ k_fp8_gemm(const Fp8TileArgs p) {
     static_assert(DEPTH >= 1 && GS >= DEPTH, "a group of scales is older than the codes that the wait leaves in flight");
     static_assert(FM * FN % 4 == 0 && FN % 2 == 0, "the sums in flight, and the fragments of weights, go round");
 
+    // both lines of the arguments before anything is made of either: one latency of memory, not two in a row (0.1 to 0.2 us)
+    asm volatile("" ::"s"(p.qx), "s"(p.tiles_m));
     extern __shared__ __align__(1024) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int w = wave % NWW, ks = wave / NWW, wm = w / WGN, wn = w % WGN;
@@ -360,11 +362,12 @@ k_fp8_gemm(const Fp8TileArgs p) {
         __syncthreads();
     }
 
-    // ---- epilogue: element e of block (i, j) is token m0 + wm WM + 16 i + r16, channel n0 + wn WO + 16 j + 4 kg + e.  The 16 tokens of a
-    // group go through LDS (private to the wave) into 16-byte pieces of rows.
-    constexpr int SLAB = 16 * WO * 2;
-    static_assert(NWW * KS * SLAB <= NSTAGE * STAGE, "the slabs go through the stages");
-    unsigned char* slab = smem + wave * SLAB;
+    // ---- epilogue: element e of block (i, j) is token m0 + wm WM + 16 i + r16, channel n0 + wn WO + 16 j + 4 kg + e.  A wave's outputs go
+    // through LDS of its own into 16-byte pieces of rows, 16-byte chunk c of row r at position c ^ swz(r).  Only the registers' way into LDS is
+    // written out; the stores are a loop, since code that runs once comes from memory (256 x 256, one K block: 13.0 us with all of it written out).
+    constexpr int WR = WM / KS, CPS = WO / 8, RPB = WO < 128 ? 128 / WO : 1;      // the wave's rows, a row's chunks, rows of all the banks
+    static_assert(FM % KS == 0 && BM * BO * 2 <= NSTAGE * STAGE, "the outputs go through the stages");
+    unsigned char* slab = smem + wave * (WR * WO * 2);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         if (i % KS != ks) continue;
@@ -375,24 +378,29 @@ k_fp8_gemm(const Fp8TileArgs p) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = silu(v[e]) * acc[i][j + FO][e];
             }
-            *reinterpret_cast<u32x2*>(slab + r16 * (WO * 2) + (16 * j + 4 * kg) * 2) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            *reinterpret_cast<u32x2*>(slab + (16 * (i / KS) + r16) * (WO * 2) + (((2 * j + (kg >> 1)) ^ ((r16 / RPB) & (CPS - 1))) << 4) + 8 * (kg & 1)) =
+                u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        const int tbase = m0 + wm * WM + 16 * i, nbase = n0 + wn * WO;
-        constexpr int CPS = WO / 8;
-#pragma unroll
-        for (int c = lane; c < 16 * CPS; c += 64) {
-            const int row = c / CPS, col = (c % CPS) * 8;
-            const uint16_t* from = reinterpret_cast<const uint16_t*>(slab + row * (WO * 2) + col * 2);
-            uint16_t* to = p.y + (int64_t)(tbase + row) * p.ldo + nbase + col;
-            if (tbase + row < p.T) {
-                // 16 bytes wherever they lie: the memory system takes wide accesses at any address
-                if (nbase + col + 8 <= p.N) __builtin_memcpy(to, from, 16);
-                else
-                    for (int e = 0; nbase + col + e < p.N; ++e) to[e] = from[e];
-            }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const int n = n0 + wn * WO + lane % CPS * 8;
+#pragma unroll 4
+    for (int row = lane / CPS; row < WR; row += 64 / CPS) {
+        const int t = m0 + wm * WM + 16 * (row / 16 * KS + ks) + row % 16;
+        const uint16_t* from = reinterpret_cast<const uint16_t*>(slab + row * (WO * 2) + ((lane % CPS ^ ((row % 16 / RPB) & (CPS - 1))) << 4));
+        uint16_t* to = p.y + (int64_t)t * p.ldo + n;
+        // 16 bytes wherever they lie: the memory system takes wide accesses at any address
+        if (t < p.T && n + 8 <= p.N) __builtin_memcpy(to, from, 16);
+    }
+    if (n < p.N && n + 8 > p.N) {
+#pragma unroll 1
+        for (int row = lane / CPS; row < WR; row += 64 / CPS) {
+            const int t = m0 + wm * WM + 16 * (row / 16 * KS + ks) + row % 16;
+            const uint16_t* from = reinterpret_cast<const uint16_t*>(slab + row * (WO * 2) + ((lane % CPS ^ ((row % 16 / RPB) & (CPS - 1))) << 4));
+            if (t < p.T)
+#pragma unroll 1
+                for (int e = 0; n + e < p.N; ++e) p.y[(int64_t)t * p.ldo + n + e] = from[e];
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }
 
