@@ -440,19 +440,19 @@ struct Tile {
     double cost[8];
 };
 const Tile kTiles[] = {
-    {8, 16, {2.702, 0.6983, 0.03768, 0.003744, 0.0113, 0.02465, 0.0393, 1.426}},
-    {16, 16, {2.688, 0.633, 0.04021, 0.009271, 0.01378, 0.03138, 0.0344, 1.541}},
-    {8, 32, {2.767, 0.6047, 0.05988, 4.597e-05, 0.01609, 0.03863, 0.05071, 2.208}},
-    {16, 32, {2.66, 0.3586, 0.0711, 0.01032, 0.02225, 0.04378, 0.04695, 0.8711}},
-    {32, 32, {3.067, 0.6569, 0.09402, 0.002435, 0.02258, 0.06412, 0.0434, 0.8417}},
-    {64, 32, {3.719, 2.038, 0.1343, 0.005339, 0.00823, 0.1374, 0.03797, 0.6391}},
-    {64, 64, {3.582, 1.983, 0.175, 0, 0.03284, 0.1652, 0.05286, 0.4602}},
-    {64, 64, {2.869, 0.6223, 0.245, 0, 0.1342, 0.05396, 0.05734, 0.296}},
-    {64, 128, {3.429, 1.849, 0.3045, 0, 0.08042, 0.2688, 0.05823, 0.2737}},
-    {128, 128, {5.033, 2.679, 0.417, 0.03609, 0.1424, 0.4384, 0.03079, 0.2732}},
-    {128, 128, {5.001, 1.272, 0.4872, 0.02605, 0.2506, 0.2602, 0.02463, 0.2591}},
-    {128, 256, {6.824, 4.51, 0.6414, 0.09983, 0.2602, 0.7028, 0.0318, 0.1967}},
-    {256, 256, {11.7, 7.193, 1.065, 0.3435, 0.5567, 1.191, 0, 0.2222}},
+    {8, 16, {2.696, 0.6948, 0.0376, 0.003804, 0.01109, 0.02497, 0.03937, 1.578}},
+    {16, 16, {2.677, 0.6307, 0.04023, 0.009718, 0.01423, 0.03093, 0.03426, 1.634}},
+    {8, 32, {2.734, 0.5718, 0.05993, 0.0001506, 0.0156, 0.03934, 0.05048, 2.667}},
+    {16, 32, {2.633, 0.3302, 0.07102, 0.01027, 0.0214, 0.04488, 0.0468, 1.053}},
+    {32, 32, {3.063, 0.6422, 0.09365, 0.003589, 0.02283, 0.06409, 0.04334, 0.8272}},
+    {64, 32, {3.683, 1.983, 0.1344, 0.006331, 0.008033, 0.1389, 0.03713, 0.5888}},
+    {64, 64, {3.328, 1.687, 0.1716, 0.0007186, 0.03206, 0.1666, 0.05376, 0.5}},
+    {64, 64, {2.627, 0.4282, 0.2324, 0, 0.1255, 0.06432, 0.05639, 0.3038}},
+    {64, 128, {3.056, 1.47, 0.2918, 0, 0.07068, 0.2674, 0.05896, 0.2557}},
+    {128, 128, {3.697, 1.589, 0.3721, 0.02714, 0.1339, 0.4102, 0.03928, 0.2679}},
+    {128, 128, {3.731, 0.402, 0.467, 0.03458, 0.2668, 0.2518, 0.02569, 0.2271}},
+    {128, 256, {4.366, 2.152, 0.6234, 0.1061, 0.2853, 0.6835, 0.03302, 0.2263}},
+    {256, 256, {6.545, 3.155, 1.089, 0.3802, 0.5706, 1.188, 0, 0.2507}},
 };
 constexpr int kNumTiles = sizeof(kTiles) / sizeof(kTiles[0]);
 
