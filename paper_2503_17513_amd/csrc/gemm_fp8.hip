@@ -9,8 +9,8 @@
 // 7 2^-13 of a run's largest product, an eightieth of what a code's own rounding (2^-4) leaves.
 //
 // What bounds it: the instruction alone runs at 4270 TFLOP/s, with the FMAs, which share its issue slots, at 3450 (32 x 32 x 64: 3890 and
-// 3360, for twice the sums in flight), registers only; 4096 x 14336 x 4096 (tokens, features, channels, here and below) runs at 2530 (190 us),
-// an unscaled library product at 2690.  There the matrix pipe is busy 72 % of the cycles at a clock that power holds at 1.5 to 1.9 GHz.
+// 3360, for twice the sums in flight), registers only; 4096 x 14336 x 4096 (tokens, features, channels, here and below) runs at 2570 (187 us),
+// an unscaled library product at 2690.  There the matrix pipe is busy 73 % of the cycles at a clock that power holds at 1.5 to 1.9 GHz.
 #include "gemm_fp8.h"
 
 #include <algorithm>
@@ -59,11 +59,11 @@ k_fp8_gemm_generic(const uint8_t* __restrict__ qx, const float* __restrict__ sx,
 // a token: one sx a lane, one sw a wave.
 //
 // Two schedules, by what fits the registers.  AHEAD (up to 128 x 128): a step's operands are all in registers when it begins; a step costs
-// one wait and one barrier.  333 x 4096 x 4096 on 64 x 128: 13.0 to 13.9 us, 0.34 a step, of which 0.11 are matrix instructions of its two waves a
-// SIMD; the rest is the issue of 60 to 75 other instructions a wave (16 FMAs, 10 LDS reads, DMA, addresses, waits).  Rings of 5 and 6 stages,
-// waves of twice the tile and two slices of K are no faster (14.1 to 16.9).
+// one wait and one barrier.  333 x 4096 x 4096 on 64 x 128: 13.1 us, 0.29 a step, of which 0.11 are matrix instructions of its two waves a
+// SIMD.  A wave spends 41 % of its time at waits and the barrier, 27 % ready for a slot and 32 % issuing some 60 instructions a step; rings of 5 and 6
+// stages, waves of twice the tile, two slices of K, and operands straight from L2 into registers (16 rows a load: 32) are no faster.
 // Not AHEAD (128 x 128 to 256 x 256, two workgroups a compute unit where they fit): stages in two parts, described there.  256 x 256: half the
-// bytes from L2 and LDS for an operation, and with them less power: 4096 x 14336 x 4096 189 us, on 128 x 256 223, on 128 x 128 249 (AHEAD 268).
+// bytes from L2 and LDS for an operation, and with them less power: 4096 x 14336 x 4096 187 us, on 128 x 256 219, on 128 x 128 247 (AHEAD 265).
 constexpr int fp8_stage(int bm, int bn, int ks) { return ks * (bm + bn) * 128; }
 constexpr int fp8_scale_blocks(int bm, bool gated) { return (bm + 63) / 64 + (gated ? 2 : 1); }
 constexpr int fp8_lds(int bm, int bn, int ks, int nstage, bool gated) { return nstage * fp8_stage(bm, bn, ks) + 2 * 1024 * fp8_scale_blocks(bm, gated); }
@@ -364,7 +364,7 @@ k_fp8_gemm(const Fp8TileArgs p) {
 
     // ---- epilogue: element e of block (i, j) is token m0 + wm WM + 16 i + r16, channel n0 + wn WO + 16 j + 4 kg + e.  A wave's outputs go
     // through LDS of its own into 16-byte pieces of rows, 16-byte chunk c of row r at position c ^ swz(r).  Only the registers' way into LDS is
-    // written out; the stores are a loop, since code that runs once comes from memory (256 x 256, one K block: 13.0 us with all of it written out).
+    // written out; the stores are a loop, since code that runs once comes from memory (256 x 256, one K block: 7.0 us, 13.0 with all of it written out).
     constexpr int WR = WM / KS, CPS = WO / 8, RPB = WO < 128 ? 128 / WO : 1;      // the wave's rows, a row's chunks, rows of all the banks
     static_assert(FM % KS == 0 && BM * BO * 2 <= NSTAGE * STAGE, "the outputs go through the stages");
     unsigned char* slab = smem + wave * (WR * WO * 2);
@@ -434,7 +434,7 @@ int g_fp8_tile_override = 0;
 
 // The tiles, and their times by tile_cost: fitted, in us, to 2600 shapes of 1 .. 4096 tokens, 256 .. 16384 features and 128 .. 14336 channels, a
 // third of them gated, up to 256 tokens the geometric mean of weights from the caches and from memory (a fit's mean error is 3 to 7 %).  On
-// these shapes the tile of the least estimate is 0.4 % slower in the mean than the fastest of all that were timed, 2.4 % at the 95th percentile.
+// these shapes the tile of the least estimate is 0.3 % slower in the mean than the fastest of all that were timed, 1.9 % at the 95th percentile.
 struct Tile {
     int rows, weights;           // of the tile: tokens, weights (of both matrices where gated)
     double cost[8];
@@ -512,7 +512,8 @@ pme_status launch_fp8_gemm_mfma(const Fp8GemmArgs& a) {
     double us = 0;
     const int id = choose(a, &us);
     // A large tile whose last round would fill few compute units: the whole rounds by it, and the channels that are left by what is fastest
-    // for them, where that is estimated a twentieth better at least (gated 1999 x 14336 x 4096 229 -> 226 us, 700 x 14336 x 4096 108 -> 97).
+    // for them, where that is estimated a twentieth better at least (gated 1999 x 4096 x 14336 221 -> 215 us, 700 x 4096 x 14336 98 -> 93, 2337 x 7680 x
+    // 3456 146 -> 126).
     int first_id = -1, rest_id = -1;
     int64_t first = 0;
     us *= 0.95;
