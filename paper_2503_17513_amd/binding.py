@@ -331,7 +331,9 @@ _device_here = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 def _stream_here(*tensors) -> int:
     """The current stream, of the device that all of `tensors` have to be on."""
-    dev = _device_here() if tensors[0].is_cuda else -2
+    dev = tensors[0].get_device()
+    if dev < 0 or dev != _device_here():
+        dev = -2
     for t in tensors:
         if t.get_device() != dev:
             raise ValueError("every operand must be a tensor of the current device")
@@ -340,9 +342,10 @@ def _stream_here(*tensors) -> int:
 
 def _matrix(x: torch.Tensor):
     """As _rows, with fewer calls (the host's share of the smallest calls is most of them)."""
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError("a [rows, d] matrix is required")
-    (rows, d), (ld, unit) = x.shape, x.stride()
+    (rows, d), (ld, unit) = shape, x.stride()
     if unit != 1:
         raise ValueError("a matrix must have unit stride along its rows")
     return rows, d, ld if rows > 1 or ld > d else d
@@ -414,9 +417,10 @@ def quantize_weights_fp8(wt: torch.Tensor, qw: torch.Tensor | None = None, sw: t
 
 
 def _fp8_operand(q, s, what: str, per: int):
-    if q.dtype != _FP8 or q.dim() != 2 or not q.is_contiguous() or q.shape[1] % FP8_BLOCK:
+    shape = q.shape
+    if q.dtype != _FP8 or len(shape) != 2 or shape[1] % FP8_BLOCK or not q.is_contiguous():
         raise ValueError(f"q{what} must be a contiguous float8_e4m3fn tensor with rows of whole groups of 128")
-    rows, K = q.shape
+    rows, K = shape
     if s.dtype != torch.float32 or s.shape != ((rows + per - 1) // per, K // FP8_BLOCK) or not s.is_contiguous():
         raise ValueError(f"s{what} must be a contiguous float32 tensor with one scale for each block of q{what}")
     return rows, K

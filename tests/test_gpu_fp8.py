@@ -387,6 +387,44 @@ def test_scales_that_are_not_finite_reach_their_rows_and_channels_only(tile):
             assert torch.equal(y[~bad], clean[~bad])
 
 
+def test_gate_over_its_range():
+    """g = u = the token's scale: half a step of bf16, eight of fp32's roundings, and what a reciprocal below 2^-126 may lose."""
+    g = torch.cat([torch.linspace(-130.0, 130.0, 2601), torch.tensor([0.0, 1e-30, -1e-30, 1e15, -1e15, -87.3, -88.0, -88.8])]).cuda()[:, None]
+    x = torch.zeros((len(g), 128), device="cuda")
+    x[:, 5] = 1.0
+    x, w, one = x.to(torch.float8_e4m3fn), x[:300].to(torch.float8_e4m3fn), torch.ones((3, 1), device="cuda")
+    v = _f64(g)
+    with np.errstate(over="ignore"):
+        ref = v / (1 + np.exp(-v)) * v
+    for tile in (0, 203, 204, 205, 206, 207, 208, 209, 210, 211, 212, 213):
+        pme.set_gemm_tile(tile)
+        y = pme.fp8_gated_gemm(x, g, w, one, w, one)
+        torch.cuda.synchronize()
+        # bf16's numbers are 2^-133 apart below 2^-126: half of that is lost where 1e-30 comes out as 5e-61, which no bf16 is near
+        lim = (2.0 ** -8 + 8 * U) * np.abs(ref) + 2.0 ** -119 * np.abs(v) + 2.0 ** -134
+        err = np.abs(_f64(y) - ref)
+        assert np.all(err <= lim), (tile, v[(err > lim).any(axis=1)][:9, 0])
+    y = pme.fp8_gated_gemm(x[:1], torch.full((1, 1), float("nan"), device="cuda"), w, one, w, one)
+    torch.cuda.synchronize()
+    assert bool(torch.isnan(y).all())
+
+
+@pytest.mark.parametrize("tile", [0, *TILES])
+def test_rows_and_blocks_of_channels_of_larger_operands(tile):
+    """Views of tokens and of blocks of channels: scales aligned to 4 bytes only where a row has an odd number of them, codes to 16 and more."""
+    ops = _operands(70, 640, 400, 21, mats=2)
+    view = [ops[0][3:], ops[1][3:], ops[2][128:], ops[3][1:], ops[4][128:], ops[5][1:]]
+    pme.set_path(pme.PATH_MFMA)
+    pme.set_gemm_tile(tile)
+    y = pme.fp8_gemm(*view[:4])
+    torch.cuda.synchronize()
+    check_gemm(y, view[:4])
+    if tile not in (201, 202):
+        z = pme.fp8_gated_gemm(*view)
+        torch.cuda.synchronize()
+        check_gated(z, view)
+
+
 # ---- together
 
 def _block(seed, T=70, d=640, f=704, f_e=768):
