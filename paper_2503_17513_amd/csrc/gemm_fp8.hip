@@ -60,9 +60,9 @@ k_fp8_gemm_generic(const uint8_t* __restrict__ qx, const float* __restrict__ sx,
 //
 // Two schedules, by what fits the registers.  AHEAD (up to 128 x 128): a step's operands are all in registers when it begins; a step costs
 // one wait and one barrier.  333 x 4096 x 4096 on 64 x 128: 13.1 us, 0.29 a step, of which 0.11 are matrix instructions of its two waves a
-// SIMD.  What bounds it are the codes' bytes through a compute unit, 80 to 85 a ns on this tile (24 KB a step), on 128 x 128 (32 KB in 0.40), on 128 x 256
-// (48 in 0.62) and on the 64 x 32 tiles that split K (48 in 0.60), on 64 units as on 192: rings of 5 and 6 stages, waves of twice the tile, two slices
-// of K, and operands straight from L2 into registers (16 rows a load: 32 us) are no faster.  Only larger tiles read less, and fill fewer units.
+// SIMD.  Codes come through a compute unit at 80 to 85 bytes a ns on this tile (24 KB a step), on 128 x 128 (32 KB in 0.40), on 128 x 256 (48 in 0.62)
+// and on the 64 x 32 tiles that split K (48 in 0.60), on 64 units as on 192, and nothing tried has raised that: rings of 5 and 6 stages, waves of twice
+// the tile, two slices of K, a ninth wave that touches the codes 5 or 10 steps ahead, operands straight from L2 into registers (16 rows a load: 32 us).
 // Not AHEAD (128 x 128 to 256 x 256, two workgroups a compute unit where they fit): stages in two parts, described there.  256 x 256: half the
 // bytes from L2 and LDS for an operation, and with them less power: 4096 x 14336 x 4096 187 us, on 128 x 256 219, on 128 x 128 247 (AHEAD 265).
 constexpr int fp8_stage(int bm, int bn, int ks) { return ks * (bm + bn) * 128; }
