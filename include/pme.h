@@ -229,8 +229,8 @@ pme_status pme_expanded_linear_mxfp4(const void* x, pme_dtype xt, int64_t T, int
  *       and must not overlap them otherwise.
  *   weight  DEVICE [d] of type wt.   eps >= 0 and finite (PME_ERR_SHAPE).
  *   qx  DEVICE out [T, Kp],  sx  DEVICE out [T, Kp / 128].
- * The sum of squares is taken in fp32, again on scaled values where it leaves fp32's range, so that values of any
- * magnitude give the quotients above (a row of zeros gives zeros).  A row that holds a NaN or an infinity comes out as
+ * The sum of squares is taken in fp32, again on scaled values where it or its mean with eps leaves fp32's range, so that
+ * values of any magnitude give the quotients above (a row of zeros gives zeros).  A row that holds a NaN or an infinity comes out as
  * NaN.  Alignment: x, residual, h and weight to their element size.
  */
 pme_status pme_rmsnorm_quant_fp8(const void* x, pme_dtype xt, int64_t T, int64_t d, int64_t ldx, const void* residual,

@@ -209,9 +209,9 @@ k_rmsnorm_quant_fp8(const NormQuantArgs a) {
         ss = __uint_as_float(across(__float_as_uint(wave_sum(ss)), 0, join_sum));
         const float eps = a.eps, mean = ss / (float)d;
         float pre = 1.f, rms = 1.f / sqrtf(mean + eps);
-        if (!(ss <= FLT_MAX) || mean + eps < 1e-24f) {
-            // The squares leave fp32's range (or the row holds what is not finite): again on values times a power of two that brings the
-            // larger of the largest and sqrt(eps) near 1.
+        if (!(mean + eps <= FLT_MAX) || mean + eps < 1e-24f) {
+            // The squares, or their mean with eps, leave fp32's range (or the row holds what is not finite): again on values times a power of
+            // two that brings the larger of the largest and sqrt(eps) near 1.
             uint32_t m = 0;
             for (int r = 0; r < rounds; ++r) {
 #pragma unroll

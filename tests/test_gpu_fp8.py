@@ -140,6 +140,21 @@ def test_rmsnorm_rows_beyond_the_squares_range(d):
         assert bool(torch.isnan(q[6:].float()).all()) and bool(torch.isnan(s[6:]).all())
 
 
+@pytest.mark.parametrize("d", [1, 256, 5000, 40000])
+def test_rmsnorm_mean_and_eps_that_overflow_together(d):
+    """Squares whose sum fits fp32 and an eps that fits it, while the mean and eps together do not (the last row: they do)."""
+    x = _rand((4, d), 13, dtype=torch.float32)
+    x /= x.norm(dim=1, keepdim=True)
+    for i, f in enumerate((1.8e19, 1e19, 5e17, 1.0)):   # FLT_MAX is 3.4028e38, the spacing below it 2e31
+        x[i] *= f
+    w = _rand((1, d), 14, outliers=False, dtype=torch.float32)[0]
+    for eps in (3.4028234e38, 3.4e38, 3e38):
+        q, s = pme.rmsnorm_quant_fp8(x, w, eps)
+        torch.cuda.synchronize()
+        quotient, scale = oracle.fp8_quotients(oracle.rmsnorm(_f64(x), _f64(w), np.float32(eps)))
+        check_codes(q, s, quotient, scale, norm_delta(d) + 4 * U)
+
+
 # ---- quantizers
 
 @pytest.mark.parametrize("T,d,xt", [(1, 1, "bf16"), (3, 130, "f32"), (8, 8192, "bf16"), (5, 1999, "bf16"), (2, 40001, "f32"), (1100, 4096, "bf16"), (333, 14336, "f32"), (1, 1 << 20, "bf16")])
