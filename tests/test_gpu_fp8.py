@@ -490,3 +490,51 @@ def test_block_on_another_stream_and_replayed():
         eager = _run_block(b, b["r"] * (k + 1))
         torch.cuda.synchronize()
         assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(eager, out))
+
+
+# ---- more rows than a grid has workgroups for: each takes further ones
+
+@pytest.mark.parametrize("xt", ["bf16", "f32"])
+def test_quant_rows_beyond_the_grid(xt):
+    cap, T, d = 1 << 15, (1 << 16) + 70, 130
+    x = torch.randn((T, d), device="cuda", generator=torch.Generator("cuda").manual_seed(1)).to(DT[xt])
+    q, s = pme.quant_fp8(x)
+    parts = [pme.quant_fp8(x[i:i + cap]) for i in range(0, T, cap)]
+    torch.cuda.synchronize()
+    assert torch.equal(q.view(torch.uint8), torch.cat([p[0].view(torch.uint8) for p in parts])) and torch.equal(s, torch.cat([p[1] for p in parts]))
+    at = [0, cap - 1, cap, cap + 1, 2 * cap, T - 1]
+    check_codes(q.view(torch.uint8)[at].view(q.dtype), s[at], *oracle.fp8_quotients(_f64(x[at])), 0.0)
+
+
+# a wave, several waves with one chunk a lane, and with two, for a row
+@pytest.mark.parametrize("cap,d,residual", [(1 << 22, 8, True), (1 << 20, 520, True), (1 << 20, 1544, False)])
+def test_rmsnorm_rows_beyond_the_grid(cap, d, residual):
+    T, gen = cap + 3000, torch.Generator("cuda").manual_seed(2)      # (the rows behind go by themselves on the same kernel)
+    x = torch.randn((T, d), device="cuda", generator=gen, dtype=torch.bfloat16)
+    r = torch.randn((T, d), device="cuda", generator=gen, dtype=torch.bfloat16) if residual else None
+    x[cap + 2000] *= 1e30                             # squares that overflow: the row's further sums, on the other of its two places
+    w = torch.randn((d,), device="cuda", generator=gen)
+    whole = pme.rmsnorm_quant_fp8(x, w, EPS, r)
+    parts = [pme.rmsnorm_quant_fp8(x[i:j], w, EPS, r[i:j] if residual else None) for i, j in ((0, cap), (cap, T))]
+    torch.cuda.synchronize()
+    for got, *want in zip(whole, *parts):
+        got, want = got.view(torch.uint8), torch.cat([t.view(torch.uint8) for t in want])
+        assert torch.equal(got, want)
+    at = [0, cap - 1, cap, cap + 1, cap + 2000, T - 1]
+    h = (x[at].float() + r[at].float()).to(torch.bfloat16) if residual else x[at]
+    if residual:
+        assert torch.equal(whole[2][at], h)
+    check_codes(whole[0].view(torch.uint8)[at].view(whole[0].dtype), whole[1][at], *oracle.fp8_quotients(oracle.rmsnorm(_f64(h), _f64(w), EPS)), norm_delta(d) + 4 * U)
+
+
+def test_weight_blocks_beyond_the_grid():
+    cap, d = 128 << 15, 130
+    N = cap + 300
+    w = torch.randn((N, d), device="cuda", generator=torch.Generator("cuda").manual_seed(3), dtype=torch.bfloat16)
+    w[cap - 128:cap] *= 100.0                         # neighbouring blocks of other scales
+    w[cap + 128:cap + 256] *= 0.01
+    q, s = pme.quantize_weights_fp8(w)
+    parts = [pme.quantize_weights_fp8(w[:cap]), pme.quantize_weights_fp8(w[cap:])]
+    torch.cuda.synchronize()
+    assert torch.equal(q.view(torch.uint8), torch.cat([p[0].view(torch.uint8) for p in parts])) and torch.equal(s, torch.cat([p[1] for p in parts]))
+    check_codes(q[cap - 128:], s[(cap - 128) // 128:], *oracle.fp8_quotients_weights(_f64(w[cap - 128:])), 0.0)
