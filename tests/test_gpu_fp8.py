@@ -538,3 +538,63 @@ def test_weight_blocks_beyond_the_grid():
     torch.cuda.synchronize()
     assert torch.equal(q.view(torch.uint8), torch.cat([p[0].view(torch.uint8) for p in parts])) and torch.equal(s, torch.cat([p[1] for p in parts]))
     check_codes(q[cap - 128:], s[(cap - 128) // 128:], *oracle.fp8_quotients_weights(_f64(w[cap - 128:])), 0.0)
+
+
+_COLD_SCRIPT = """
+import sys, torch
+sys.path.insert(0, sys.argv[1])
+import paper_2503_17513_amd as pme
+FP8, gen = torch.float8_e4m3fn, torch.Generator("cuda").manual_seed(5)
+def codes(rows, K):
+    return (torch.randn((rows, K), device="cuda", generator=gen) * 100).clamp(-448, 448).to(FP8)
+def scales(rows, K):
+    return torch.rand((rows, K // 128), device="cuda", generator=gen) * 1e-3
+T, K, N = 70, 640, 300
+x, r, w = torch.randn((T, 600), device="cuda", generator=gen), torch.randn((T, 600), device="cuda", generator=gen), torch.ones(600, device="cuda")
+wide = torch.randn((3, 40000), device="cuda", generator=gen).to(torch.bfloat16)
+wide_w = torch.ones(40000, device="cuda", dtype=torch.bfloat16)
+ops = [codes(T, K), scales(T, K)] + [f(n, K) for _ in range(2) for f, n in ((codes, N), (scales, 3))]
+calls = [lambda: pme.rmsnorm_quant_fp8(x, w, 1e-5, r), lambda: pme.rmsnorm_quant_fp8(wide, wide_w, 1e-5), lambda: pme.quant_fp8(x),
+         lambda: pme.quant_fp8(wide), lambda: pme.quantize_weights_fp8(x), lambda: pme.quantize_weights_fp8(wide)]
+def product(f, o, path, tile):
+    def call():
+        pme.set_path(path)
+        pme.set_gemm_tile(tile)
+        y = f(*o)
+        pme.set_gemm_tile(0)
+        pme.set_path(pme.PATH_AUTO)
+        return [y]
+    return call
+for f, o in ((pme.fp8_gemm, ops[:4]), (pme.fp8_gated_gemm, ops)):
+    calls.append(product(f, o, pme.PATH_GENERIC, 0))
+    calls.append(product(f, o, pme.PATH_AUTO, 0))
+    for tile in range(201 if f is pme.fp8_gemm else 203, 214):
+        calls.append(product(f, o, pme.PATH_MFMA, tile))
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph, stream=torch.cuda.Stream()):      # the process's first call of every one of them
+    out = [[t.view(torch.uint8) for t in call()] for call in calls]
+for _ in range(3):
+    for ts in out:
+        for t in ts:
+            t.fill_(0xA5)
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    got = [[t.clone() for t in ts] for ts in out]
+    want = [[t.view(torch.uint8) for t in call()] for call in calls]
+    torch.cuda.synchronize()
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert all(torch.equal(p, q) for p, q in zip(a, b)), i
+print("COLD_OK", len(calls))
+"""
+
+
+def test_first_calls_of_all_kernels_are_captured():
+    # in a process of its own: here every kernel has run
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    p = subprocess.run([sys.executable, "-c", _COLD_SCRIPT, root], capture_output=True, text=True, timeout=110)
+    assert p.returncode == 0 and "COLD_OK 34" in p.stdout, p.stdout[-2000:] + p.stderr[-2000:]
