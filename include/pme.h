@@ -337,7 +337,7 @@ void pme_set_gemm_tile(int id);
 pme_status pme_gemm_plan(int variant, int64_t T, int64_t d_e, int64_t N, char* name, size_t name_len);
 
 /* The same of pme_fp8_gemm (gated = 0) and pme_fp8_gated_gemm (gated != 0); where two kernels share the channels, the
- * one of the first channels. */
+ * one of the first channels; where operands go in slices (beyond 4 GiB), the first slice's. */
 pme_status pme_fp8_gemm_plan(int gated, int64_t T, int64_t K, int64_t N, char* name, size_t name_len);
 
 void pme_set_path(pme_path p);

@@ -223,7 +223,7 @@ pme_status run_fp8_gemm(const pme::Fp8GemmArgs& a) {
             }
             p.y = static_cast<unsigned char*>(a.y) + (t0 * a.ldy + n0) * 2;
             const pme_status s = run_fp8_gemm_slice(p);
-            if (s != PME_OK) return s;
+            if (s != PME_OK || a.dry) return s;             // a dry run is about the first slice
         }
     return PME_OK;
 }

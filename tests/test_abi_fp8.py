@@ -83,6 +83,14 @@ def test_fp8_gemm_plan_by_fitted_times(T, K, N, gated, kernel):
     assert pme.fp8_gemm_plan(T, K, N, gated=gated).startswith(kernel)
 
 
+# operands beyond 4 GiB go in slices of 299520 rows of 14336 codes, or of 3840 rows of 2^20
+@pytest.mark.parametrize("T,K,N,first,gated", [(300032, 14336, 72, (299520, 14336, 72), False), (200, 14336, 300032, (200, 14336, 299520), True),
+                                               (1 << 24, 1 << 20, 1 << 20, (3840, 1 << 20, 3840), False)])
+def test_fp8_gemm_plan_names_the_kernel_of_the_first_slice(T, K, N, first, gated):
+    assert pme.fp8_gemm_plan(T, K, N, gated=gated) == pme.fp8_gemm_plan(*first, gated=gated)
+    assert pme.fp8_gemm_plan(T, K, N, gated=gated) != pme.fp8_gemm_plan(T % first[0] or T, K, N % first[2] or N, gated=gated)
+
+
 def test_a_forced_fp8_tile_that_refuses_is_not_replaced():
     f, buf = pme.lib().pme_fp8_gemm_plan, C.create_string_buffer(96)
     try:
