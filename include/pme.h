@@ -340,6 +340,10 @@ pme_status pme_gemm_plan(int variant, int64_t T, int64_t d_e, int64_t N, char* n
  * one of the first channels; where operands go in slices (beyond 4 GiB), the first slice's. */
 pme_status pme_fp8_gemm_plan(int gated, int64_t T, int64_t K, int64_t N, char* name, size_t name_len);
 
+/* The second of those two kernels: *first (HOST out) is its first channel, name (HOST out) its name; N and "" where one
+ * kernel computes all channels. */
+pme_status pme_fp8_gemm_rest(int gated, int64_t T, int64_t K, int64_t N, int64_t* first, char* name, size_t name_len);
+
 void pme_set_path(pme_path p);
 pme_path pme_get_path(void);
 const char* pme_status_string(pme_status s);

@@ -18,7 +18,7 @@ EXPORTS = ("pme_hadamard_expand_quant", "pme_expand_quantize_weights", "pme_hada
            "pme_mxfp4_gemm", "pme_expanded_linear_mxfp4", "pme_hadamard_expand_quant_asym", "pme_w4a4_gemm", "pme_w4a4_gemm_asym",
            "pme_weight_rowsum", "pme_expanded_linear", "pme_expanded_linear_static", "pme_expanded_linear_asym", "pme_workspace_bytes", "pme_hadamard_expand_f32",
            "pme_w4a4_gemm_i32", "pme_factor_order", "pme_base_block", "pme_pack_int4", "pme_gemm_plan", "pme_probe_copy", "pme_probe_read", "pme_probe_launch", "pme_probe_mfma",
-           "pme_rmsnorm_quant_fp8", "pme_quant_fp8", "pme_quantize_weights_fp8", "pme_fp8_gemm", "pme_fp8_gated_gemm", "pme_fp8_gemm_plan",
+           "pme_rmsnorm_quant_fp8", "pme_quant_fp8", "pme_quantize_weights_fp8", "pme_fp8_gemm", "pme_fp8_gated_gemm", "pme_fp8_gemm_plan", "pme_fp8_gemm_rest",
            "pme_set_path", "pme_set_gemm_tile",
            "pme_get_path", "pme_status_string", "pme_version")
 
@@ -68,6 +68,7 @@ def lib() -> C.CDLL:
     L.pme_fp8_gemm.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, i64, vp]
     L.pme_fp8_gated_gemm.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, i64, vp]
     L.pme_fp8_gemm_plan.argtypes = [i32, i64, i64, i64, C.c_char_p, sz]
+    L.pme_fp8_gemm_rest.argtypes = [i32, i64, i64, i64, C.POINTER(C.c_int64), C.c_char_p, sz]
     L.pme_probe_copy.argtypes = [vp, vp, sz, vp]
     L.pme_probe_read.argtypes = [vp, sz, vp, sz, vp]
     L.pme_probe_launch.argtypes = [vp]
@@ -468,6 +469,13 @@ def fp8_gemm_plan(T: int, K: int, N: int, gated: bool = False) -> str:
     buf = C.create_string_buffer(128)
     _check(lib().pme_fp8_gemm_plan(int(gated), T, K, N, buf, len(buf)), "pme_fp8_gemm_plan")
     return buf.value.decode()
+
+
+def fp8_gemm_rest(T: int, K: int, N: int, gated: bool = False) -> tuple[int, str]:
+    """Where a second kernel takes the channels behind whole rounds of fp8_gemm_plan's: the first of them, and its name; (N, "") elsewhere."""
+    first, buf = C.c_int64(), C.create_string_buffer(128)
+    _check(lib().pme_fp8_gemm_rest(int(gated), T, K, N, C.byref(first), buf, len(buf)), "pme_fp8_gemm_rest")
+    return first.value, buf.value.decode()
 
 
 STATIC_SCRATCH_BYTES = 16 << 20

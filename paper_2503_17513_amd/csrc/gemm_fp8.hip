@@ -531,7 +531,11 @@ pme_status launch_fp8_gemm_mfma(const Fp8GemmArgs& a) {
     }
     if (first_id < 0) return launch_id(a, id);
     const pme_status s = launch_id(channels_of(a, 0, first), first_id);
-    return s != PME_OK || a.dry ? s : launch_id(channels_of(a, first, a.N - first), rest_id);
+    if (s != PME_OK) return s;
+    Fp8GemmArgs rest = channels_of(a, first, a.N - first);
+    rest.plan = a.rest_plan;
+    if (a.rest) *a.rest = first;
+    return launch_id(rest, rest_id);
 }
 
 pme_status launch_fp8_gemm_generic(const Fp8GemmArgs& a) {

@@ -228,6 +228,21 @@ pme_status run_fp8_gemm(const pme::Fp8GemmArgs& a) {
     return PME_OK;
 }
 
+// A dry run of a product: the names of its kernels, and the first channel of the second (N where one computes all).
+pme_status plan_fp8_gemm(int gated, int64_t T, int64_t K, int64_t N, const char** plan, int64_t* rest, const char** rest_plan) {
+    // operands as a caller's allocations are: 256-byte aligned, never dereferenced by a dry run
+    const uint8_t* p8 = reinterpret_cast<const uint8_t*>(uintptr_t(256));
+    const float* pf = reinterpret_cast<const float*>(uintptr_t(256));
+    pme::Fp8GemmArgs a{p8, pf, p8, pf, gated ? p8 : nullptr, gated ? pf : nullptr, T, K, N, const_cast<uint8_t*>(p8), N, nullptr};
+    a.dry = true;
+    a.plan = plan;
+    a.rest = rest;
+    a.rest_plan = rest_plan;
+    const pme_status st = check_fp8_gemm(a, gated != 0);
+    if (st != PME_OK) return st;
+    return T == 0 || N == 0 ? PME_ERR_SHAPE : run_fp8_gemm(a);
+}
+
 // A quantizer's input of rows x d values and its codes and scales.
 pme_status check_quant_fp8(const void* x, pme_dtype xt, int64_t rows, int64_t d, int64_t ldx, const uint8_t* q, const float* s) {
     if (xt != PME_F32 && xt != PME_BF16) return PME_ERR_DTYPE;
@@ -521,17 +536,20 @@ pme_status pme_fp8_gated_gemm(const uint8_t* qx, const float* sx, const uint8_t*
 
 pme_status pme_fp8_gemm_plan(int gated, int64_t T, int64_t K, int64_t N, char* name, size_t name_len) {
     if (!name || name_len == 0) return PME_ERR_NULL;
-    // operands as a caller's allocations are: 256-byte aligned, never dereferenced by a dry run
-    const uint8_t* p8 = reinterpret_cast<const uint8_t*>(uintptr_t(256));
-    const float* pf = reinterpret_cast<const float*>(uintptr_t(256));
     const char* plan = "";
-    pme::Fp8GemmArgs a{p8, pf, p8, pf, gated ? p8 : nullptr, gated ? pf : nullptr, T, K, N, const_cast<uint8_t*>(p8), N, nullptr};
-    a.dry = true;
-    a.plan = &plan;
-    pme_status st = check_fp8_gemm(a, gated != 0);
-    if (st == PME_OK && (T == 0 || N == 0)) st = PME_ERR_SHAPE;
-    if (st != PME_OK || (st = run_fp8_gemm(a)) != PME_OK) return st;
-    snprintf(name, name_len, "%s", plan);
+    const pme_status st = plan_fp8_gemm(gated, T, K, N, &plan, nullptr, nullptr);
+    if (st == PME_OK) snprintf(name, name_len, "%s", plan);
+    return st;
+}
+
+pme_status pme_fp8_gemm_rest(int gated, int64_t T, int64_t K, int64_t N, int64_t* first, char* name, size_t name_len) {
+    if (!first || !name || name_len == 0) return PME_ERR_NULL;
+    const char *plan = "", *rest_plan = "";
+    int64_t rest = N;
+    const pme_status st = plan_fp8_gemm(gated, T, K, N, &plan, &rest, &rest_plan);
+    if (st != PME_OK) return st;
+    *first = rest;
+    snprintf(name, name_len, "%s", rest_plan);
     return PME_OK;
 }
 

@@ -146,6 +146,9 @@ struct Fp8GemmArgs {
     hipStream_t stream;
     bool dry = false;    // only answer whether a kernel takes the shape: nothing is launched
     const char** plan = nullptr;   // dry runs: receives the name of the kernel configuration that would run
+    // ... and, where a second kernel takes the channels behind whole rounds of it, the first of these and that kernel's name
+    int64_t* rest = nullptr;
+    const char** rest_plan = nullptr;
 };
 pme_status launch_fp8_gemm_generic(const Fp8GemmArgs& a);
 pme_status launch_fp8_gemm_mfma(const Fp8GemmArgs& a);

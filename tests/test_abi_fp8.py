@@ -73,6 +73,26 @@ def test_fp8_gemm_plan_argument_errors():
     assert f(1, 4, 256, 8, buf, 64) == OK and buf.value.startswith(b"k_fp8_")
 
 
+def test_fp8_gemm_rest():
+    f, buf, first = pme.lib().pme_fp8_gemm_rest, C.create_string_buffer(64), C.c_int64(-5)
+    at = C.byref(first)
+    assert f(0, 4, 256, 8, None, buf, 64) == f(0, 4, 256, 8, at, None, 64) == f(0, 4, 256, 8, at, buf, 0) == NULL
+    assert f(0, 0, 256, 8, at, buf, 64) == f(1, 4, 256, 0, at, buf, 64) == f(0, 4, 200, 8, at, buf, 64) == SHAPE
+    assert first.value == -5                                          # untouched where the call is refused
+    assert f(0, 4, 256, 8, at, buf, 64) == OK and first.value == 8 and buf.value == b""
+    first, name = pme.fp8_gemm_rest(1999, 4096, 14336, gated=True)    # 3.5 rounds of 256 x 256
+    assert first == 12288 and name.startswith("k_fp8_gemm<128, 256, ")
+    try:
+        pme.set_path(pme.PATH_GENERIC)
+        assert pme.fp8_gemm_rest(1999, 4096, 14336, gated=True) == (14336, "")
+        pme.set_path(pme.PATH_AUTO)
+        pme.set_gemm_tile(213)                                        # a forced tile computes everything
+        assert pme.fp8_gemm_rest(1999, 4096, 14336, gated=True) == (14336, "")
+    finally:
+        pme.set_gemm_tile(0)
+        pme.set_path(pme.PATH_AUTO)
+
+
 # tokens, features, channels, gated, the tile estimated fastest
 @pytest.mark.parametrize("T,K,N,gated,kernel", [
     (1, 8192, 2048, False, "k_fp8_gemm_kslice<8, 16, "), (16, 14336, 4096, False, "k_fp8_gemm_kslice<16, 16, "), (8, 2048, 8192, True, "k_fp8_gemm_kslice<16, 32, "), (2, 4096, 2048, True, "k_fp8_gemm_kslice<8, 32, "),

@@ -598,3 +598,32 @@ def test_first_calls_of_all_kernels_are_captured():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     p = subprocess.run([sys.executable, "-c", _COLD_SCRIPT, root], capture_output=True, text=True, timeout=110)
     assert p.returncode == 0 and "COLD_OK 34" in p.stdout, p.stdout[-2000:] + p.stderr[-2000:]
+
+
+# tokens, features, channels, first channel of the second kernel, gated, the first kernel and the tile that forces it
+@pytest.mark.parametrize("T,K,N,first,gated,kernel,tile,second", [
+    (396, 2048, 4142, 4096, True, "k_fp8_gemm<128, 128, 4, 2, ", 210, "k_fp8_gemm_kslice<8, 32, "), (641, 2048, 5432, 5376, False, "k_fp8_gemm<128, 128, 4, 2, ", 210, "k_fp8_gemm_kslice<16, 16, "),
+    (670, 1024, 5445, 5376, True, "k_fp8_gemm<128, 256, ", 212, "k_fp8_gemm_kslice<16, 32, "), (1288, 1024, 5908, 5888, False, "k_fp8_gemm<128, 256, ", 212, "k_fp8_gemm_kslice<16, 16, "),
+    (913, 1024, 11597, 8192, True, "k_fp8_gemm<256, 256, ", 213, "k_fp8_gemm<128, 256, "), (1426, 1152, 11767, 10752, False, "k_fp8_gemm<256, 256, ", 213, "k_fp8_gemm<64, 128, ")])
+def test_whole_rounds_on_one_kernel_and_the_rest_on_another(T, K, N, first, gated, kernel, tile, second):
+    """That two kernels run, where they meet, and both: the channels of the first as from it alone, some blocks of both against the oracle."""
+    assert pme.fp8_gemm_plan(T, K, N, gated=gated).startswith(kernel)
+    rest = pme.fp8_gemm_rest(T, K, N, gated=gated)
+    assert rest[0] == first and rest[1].startswith(second)
+    ops = _operands(T, K, N, T + N, mats=2 if gated else 1)
+    f = pme.fp8_gated_gemm if gated else pme.fp8_gemm
+    big = torch.full((T + 1, N + 3), float("nan"), dtype=torch.bfloat16, device="cuda")
+    y = f(*ops, big[:T, 1:1 + N])
+    pme.set_gemm_tile(tile)
+    assert pme.fp8_gemm_rest(T, K, N, gated=gated) == (N, "")
+    alone = f(*ops)
+    torch.cuda.synchronize()
+    assert not bool(torch.isnan(y).any()) and bool(torch.isnan(big[T]).all()) and bool(torch.isnan(big[:, [0, N + 1, N + 2]]).all())
+    assert torch.equal(y[:, :first], alone[:, :first])
+    tokens = torch.tensor(sorted({*range(16), *range(0, T, 9), *range(T - 16, T)})).cuda()
+    blocks = sorted({0, first // 128 - 1, first // 128, first // 128 + 1, (N - 1) // 128} & set(range((N + 127) // 128)))
+    rows = torch.cat([torch.arange(128 * b, min(128 * b + 128, N)) for b in blocks]).cuda()
+    part = [ops[0].view(torch.uint8)[tokens].view(torch.float8_e4m3fn), ops[1][tokens]]
+    for q, s in zip(ops[2::2], ops[3::2]):
+        part += [q.view(torch.uint8)[rows].view(torch.float8_e4m3fn), s[torch.tensor(blocks).cuda()]]
+    (check_gated if gated else check_gemm)(y[tokens][:, rows], part)
