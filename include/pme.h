@@ -214,7 +214,9 @@ pme_status pme_expanded_linear_mxfp4(const void* x, pme_dtype xt, int64_t T, int
  *
  *  - Activations: a scale for each token and 128 consecutive features; weights: one for each block of 128 output
  *    channels x 128 features.  scale = amax / 448 over the block, at least 2^-126, 1 where the block is all zeros; code =
- *    e4m3(v / scale), round half to even.  A block that holds a NaN or an infinity gets a NaN scale and NaN codes.
+ *    e4m3(v / scale), round half to even.  The scale is rounded to fp32, and the quotient by it is formed in fp32, to within 2^-22 of
+ *    itself: one that lies this near to the midpoint of two codes may become either (about one in a thousand bf16 values,
+ *    whose quotients are often midpoints; by a power of two they are exact).  A block that holds a NaN or an infinity gets a NaN scale and NaN codes.
  *  - Rows of codes are dense and hold whole blocks: Kp = 128 ceil(d / 128) bytes, the codes beyond d are 0.  Scales are
  *    dense, [rows, Kp / 128].  Codes are 16-byte aligned, scales 4-byte aligned (PME_ERR_ALIGN).
  *  - T == 0 or N == 0 is a no-op.  No call needs a workspace or a first call outside a graph's capture.  Outputs overlap

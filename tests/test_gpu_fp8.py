@@ -189,6 +189,36 @@ def test_quant_pitch_and_odd_address():
     check_codes(q, s, *oracle.fp8_quotients(_f64(x)), 0.0)
 
 
+@pytest.mark.parametrize("xt", ["bf16", "f32"])
+def test_codes_are_nearest_to_quotients_by_the_stored_scale(xt):
+    """Half a step and 2^-22 of the exact quotient by the scale that is returned: the reciprocal is rounded once behind a correction of its
+    square, and so is the product, 2 2^-24 and less than 2^-44 (twice that allowed)."""
+    x = _rand((700, 4096), 31, dtype=DT[xt])
+    for f, per in ((pme.quant_fp8, 1), (pme.quantize_weights_fp8, 128)):
+        q, s = f(x)
+        torch.cuda.synchronize()
+        quotient = _f64(x) / np.repeat(np.repeat(_f64(s), per, axis=0)[:700], 128, axis=1)
+        err = np.abs(_codes64(q) - np.clip(quotient, -448.0, 448.0)) - oracle.e4m3_step(quotient) / 2
+        assert np.all(err <= 2.0 ** -22 * np.abs(quotient)), err.max()
+
+
+def test_midpoints_go_to_the_even_code():
+    """Scales that are powers of two: all midpoints of neighbouring codes, their neighbours in fp32, and what lies below the smallest code."""
+    v = np.unique(np.abs(torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float().numpy()))
+    v = v[np.isfinite(v)].astype(np.float64)
+    assert len(v) == 127 and v[-1] == 448
+    mid = ((v[1:] + v[:-1]) / 2).astype(np.float32)
+    row = np.concatenate([mid, np.nextafter(mid, np.float32(0)), np.nextafter(mid, np.float32(1e9)), v[:-1].astype(np.float32), np.float32([1e-6, 2.0 ** -149, -0.0])])
+    row = np.concatenate([row, -row, np.zeros(-2 * len(row) % 127, np.float32)]).reshape(-1, 127)
+    row = np.concatenate([row, np.full((len(row), 1), 448.0, np.float32)], axis=1)          # every block's scale is 1
+    for p in (-20, 0, 33):
+        x = torch.from_numpy(np.ldexp(row, p)).cuda()
+        for q, s in (pme.quant_fp8(x), pme.quantize_weights_fp8(x)):
+            torch.cuda.synchronize()
+            assert bool((s == 2.0 ** p).all())
+            assert np.array_equal(_codes64(q), oracle.e4m3_round(np.ldexp(np.ldexp(row, p).astype(np.float64), -p)))
+
+
 @pytest.mark.parametrize("N,d,xt", [(1, 1, "bf16"), (127, 130, "f32"), (128, 128, "bf16"), (129, 2000, "bf16"), (300, 1024, "f32"), (2048, 257, "bf16")])
 def test_quantize_weights(N, d, xt):
     w = _rand((N, d + 3), N + d, dtype=DT[xt])[:, 1:1 + d]
