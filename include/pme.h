@@ -217,8 +217,9 @@ pme_status pme_expanded_linear_mxfp4(const void* x, pme_dtype xt, int64_t T, int
  *    e4m3(v / scale), round half to even.  The scale is rounded to fp32, and the quotient by it is formed in fp32, to within 2^-22 of
  *    itself: one that lies this near to the midpoint of two codes may become either (about one in a thousand bf16 values,
  *    whose quotients are often midpoints; by a power of two they are exact).  A block that holds a NaN or an infinity gets a NaN scale and NaN codes.
- *  - Rows of codes are dense and hold whole blocks: Kp = 128 ceil(d / 128) bytes, the codes beyond d are 0.  Scales are
- *    dense, [rows, Kp / 128].  Codes are 16-byte aligned, scales 4-byte aligned (PME_ERR_ALIGN).
+ *  - Rows of codes are dense and hold whole blocks: Kp = 128 ceil(d / 128) bytes, the codes beyond d are 0 (NaN as the rest of
+ *    their block where its scale is).  Scales are dense, [rows, Kp / 128].  Codes are 16-byte aligned, scales 4-byte aligned
+ *    (PME_ERR_ALIGN).
  *  - T == 0 or N == 0 is a no-op.  No call needs a workspace or a first call outside a graph's capture.  Outputs overlap
  *    neither inputs nor each other, but for h below.
  */

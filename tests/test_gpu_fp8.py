@@ -181,6 +181,22 @@ def test_quant_extremes():
         assert bool(torch.isnan(s[row, 0])) and bool(torch.isnan(q[row, :128].float()).all()) and s[row, 1] == 1 and not bool(q[row, 128:].float().any())
 
 
+def test_codes_beyond_the_row():
+    """0, or NaN where their block's scale is NaN: the product is NaN for that token, and whole for the others."""
+    x = _rand((5, 200), 9, dtype=torch.float32)
+    x[1, 150], x[2, 3], x[3, 199] = float("inf"), float("nan"), float("nan")
+    w = _rand((1, 200), 10, outliers=False, dtype=torch.float32)[0]
+    for q, s, blocks in ((*pme.quant_fp8(x), [(1, 1), (2, 0), (3, 1)]), (*pme.rmsnorm_quant_fp8(x, w, EPS), [(t, b) for t in (1, 2, 3) for b in (0, 1)])):
+        bad = torch.zeros((5, 2), dtype=torch.bool, device="cuda")
+        for t, b in blocks:
+            bad[t, b] = True
+        y = pme.fp8_gemm(q, s, torch.ones((8, 256), device="cuda").to(q.dtype), torch.ones((1, 2), device="cuda"))
+        torch.cuda.synchronize()
+        assert torch.equal(torch.isnan(s), bad) and torch.equal(torch.isnan(q.float()).view(5, 2, 128).all(2), bad)
+        assert torch.equal(torch.isnan(q.float()).view(5, 2, 128).any(2), bad)
+        assert not bool(q[[0, 4], 200:].float().any()) and torch.equal(torch.isnan(y), bad.any(1, keepdim=True).expand(5, 8))
+
+
 def test_quant_pitch_and_odd_address():
     big = _rand((19, 700), 2)
     x = big[:, 5:5 + 301]
