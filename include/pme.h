@@ -249,9 +249,10 @@ pme_status pme_quantize_weights_fp8(const void* wt, pme_dtype wtype, int64_t N, 
                                     void* stream);
 
 /*
- * y[t][n] = bf16( sum_g sx[t][g] sw[n / 128][g] sum_{k in block g} qx[t][k] qw[n][k] ).  Blocks are added in fp32; inside
- * one the matrix instruction adds the products of 8 consecutive codes on a grid 13 bits below the largest exponent among
- * them, which moves such a sum by less than 7 * 2^-13 of its largest product.  PME_PATH_GENERIC adds in fp32 throughout.
+ * y[t][n] = bf16( sum_g sx[t][g] sw[n / 128][g] sum_{k in block g} qx[t][k] qw[n][k] ).  sx sw is formed
+ * first, in fp32: where it is no normal number of fp32, a sum may lose digits, vanish or come out infinite or NaN.  Blocks are added
+ * in fp32; inside one the matrix instruction adds the products of 8 consecutive codes on a grid 13 bits below the largest exponent
+ * among them, which moves such a sum by less than 7 * 2^-13 of its largest product.  PME_PATH_GENERIC adds in fp32 throughout.
  *   qx DEVICE [T, K], sx DEVICE [T, K / 128]; qw DEVICE [N, K], sw DEVICE [ceil(N / 128), K / 128]; K a multiple of 128
  *   (Kp above).  y DEVICE out [T, N] bf16 row-major, ldy elements between rows (ldy >= N), 2-byte aligned.
  */

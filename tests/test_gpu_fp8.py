@@ -448,6 +448,25 @@ def test_scales_that_are_not_finite_reach_their_rows_and_channels_only(tile):
             assert torch.equal(y[~bad], clean[~bad])
 
 
+@pytest.mark.parametrize("tile", [0, *TILES])
+def test_products_of_scales_over_fp32s_normal_range(tile):
+    """Powers of two, whose products are the smallest and the largest normal ones and some between: exact but for the sum's one bf16 rounding."""
+    x, w = torch.zeros((8, 256), device="cuda"), torch.zeros((24, 256), device="cuda")
+    x[:, 3], x[:, 130], w[:, 3], w[:, 130] = 1.0, 0.5, 0.25, 1.0      # 1/4 + 1/2 of the product of the scales
+    x, w = x.to(torch.float8_e4m3fn), w.to(torch.float8_e4m3fn)
+    pme.set_path(pme.PATH_MFMA if tile else pme.PATH_GENERIC)
+    pme.set_gemm_tile(tile)
+    for total in (-126, -20, 0, 90, 127):
+        for t in (-126, -100, -63, -1, 0, 30, 64, 127):
+            if not -126 <= total - t <= 127:
+                continue
+            sx = torch.full((8, 2), 2.0 ** t, device="cuda")
+            sw = torch.full((1, 2), 2.0 ** (total - t), device="cuda")
+            y = pme.fp8_gemm(x, sx, w, sw)
+            torch.cuda.synchronize()
+            assert bool((y.double() == 0.75 * 2.0 ** total).all()), (total, t)
+
+
 def test_gate_over_its_range():
     """g = u = the token's scale: half a step of bf16, eight of fp32's roundings, and what a reciprocal below 2^-126 may lose."""
     g = torch.cat([torch.linspace(-130.0, 130.0, 2601), torch.tensor([0.0, 1e-30, -1e-30, 1e15, -1e15, -87.3, -88.0, -88.8])]).cuda()[:, None]
