@@ -8,8 +8,8 @@
 // Rows of codes are whole groups of 128, codes beyond d are 0, so that the product knows no ragged K.
 //
 // All three are bound by HBM: the values are read once, into registers, and codes, scales and h written once (kernel times and moved bytes,
-// a plain copy of 1 GiB moves 5.2 to 5.8 TB/s: norm with a residual, 4096 x 4096 in bf16 23.7 us, 5.0 TB/s; 4096 x 14336 fp32 values 51 us,
-// 5.8; 14336 x 4096 bf16 weights 34 us, 5.2), small ones by the launch and one chain load - reduction - store (one token 2.3 us).  A lane holds chunks of
+// a plain copy of 1 GiB moves 5.2 to 5.8 TB/s: norm with a residual, 4096 x 4096 in bf16 23.7 us, 5.0 TB/s; 4096 x 14336 values 51 us in fp32,
+// 5.8, and 34 in bf16, 5.2; 14336 x 4096 bf16 weights 34 us, 5.2), small ones by the launch and one chain load - reduction - store (one token 2.3 us).  A lane holds chunks of
 // 8 consecutive values, so that a group is 16 lanes, whose largest magnitude takes four data-parallel moves; magnitudes are compared as bit
 // patterns, where infinities and NaN come out largest: their group's scale and codes are NaN.
 #include "gemm_tile.h"

@@ -60,8 +60,10 @@ k_fp8_gemm_generic(const uint8_t* __restrict__ qx, const float* __restrict__ sx,
 //
 // Two schedules, by what fits the registers.  AHEAD (up to 128 x 128): a step's operands are all in registers when it begins; a step costs
 // one wait and one barrier.  333 x 4096 x 4096 on 64 x 128: 13.1 us, 0.29 a step, of which 0.11 are matrix instructions of its two waves a
-// SIMD.  Codes come through a compute unit at 80 to 85 bytes a ns on this tile (24 KB a step), on 128 x 128 (32 KB in 0.40), on 128 x 256 (48 in 0.62)
-// and on the 64 x 32 tiles that split K (48 in 0.60), on 64 units as on 192, and nothing tried has raised that: rings of 5 and 6 stages, waves of twice
+// SIMD.  What holds the rest has not been told apart; two readings fit.  Codes arrive at 80 to 85 bytes a ns and unit on this tile (24 KB a step), on
+// 128 x 128 (32 KB in 0.40), on 128 x 256 (48 in 0.62) and on the 64 x 32 tiles that split K (48 in 0.60), on 64 units as on 192.  And reading the fragments
+// (64, 96 and 160 KB a step at 128 bytes a cycle of 2.4 GHz) and a constant 0.08 give 0.29, 0.40 and 0.61 on the first three; against that one, 15 %
+// fewer reads (2 x 4 waves on 128 x 256) are no faster.  Nothing tried has shortened a step: rings of 5 and 6 stages, waves of twice
 // the tile, two slices of K, a ninth wave that touches the codes 5 or 10 steps ahead, operands straight from L2 into registers (16 rows a load: 32 us).
 // Not AHEAD (128 x 128 to 256 x 256, two workgroups a compute unit where they fit): stages in two parts, described there.  256 x 256: half the
 // bytes from L2 and LDS for an operation, and with them less power: 4096 x 14336 x 4096 187 us, on 128 x 256 219, on 128 x 128 247 (AHEAD 265).
@@ -513,8 +515,8 @@ pme_status launch_fp8_gemm_mfma(const Fp8GemmArgs& a) {
     double us = 0;
     const int id = choose(a, &us);
     // A large tile whose last round would fill few compute units: the whole rounds by it, and the channels that are left by what is fastest
-    // for them, where that is estimated a twentieth better at least (gated 1999 x 4096 x 14336 221 -> 215 us, 700 x 4096 x 14336 98 -> 93, 2337 x 7680 x
-    // 3456 146 -> 126).
+    // for them, where that is estimated a twentieth better at least (gated, against the fastest tile alone: 1999 x 4096 x 14336 218 -> 212 us, 700 x 4096 x
+    // 14336 97 -> 92, 2337 x 7680 x 3456 147 -> 124).
     int first_id = -1, rest_id = -1;
     int64_t first = 0;
     us *= 0.95;
